@@ -148,8 +148,10 @@ def _quantize(x, floor):
     b, n = _to_blocks(x)
     top = b.abs().amax(-1)
     some = ~(top < _TINY)
-    scale = torch.where(some, top / _TOP, torch.zeros_like(top))
-    q = b * torch.where(some, _TOP / top, torch.zeros_like(top)).unsqueeze(-1)
+    # Tensors over tensors: where one is a number torch multiplies by a reciprocal, which rounds twice.
+    most = torch.full_like(top, _TOP)
+    scale = torch.where(some, top / most, torch.zeros_like(top))
+    q = b * torch.where(some, most / top, torch.zeros_like(top)).unsqueeze(-1)
     if floor:
         q = torch.where((q > 0) & (q < 2.0 ** -9), torch.full_like(q, 2.0 ** -9), q)
     return q.flatten(-2)[..., :n].to(torch.float8_e4m3fn).contiguous(), scale
