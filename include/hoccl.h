@@ -524,6 +524,156 @@ hoccl_status_t hoccl_ring_hop(const void *partial, const void *local, void *out,
                               size_t count, hoccl_dtype_t dtype, hoccl_hop_t hop,
                               hipStream_t stream);
 
+/* ---- operators on a rank's shard ------------------------------------------
+ * What a training step computes on a rank's shard between two collectives:
+ * AdamW between the reduce-scatter of the gradients and the all-gather of the
+ * parameters, the residual's addition with the RMS norm between the two
+ * collectives of sequence parallelism, and the router's balance loss before
+ * the all-to-all(v), whose traffic matrix its counts are.  They run as
+ * reduction kernels on the caller's stream, like hoccl_ring_hop: no copies,
+ * no allocation, no workspace of the library's (a workspace is the
+ * caller's), so calls on several streams do not wait for each other and any
+ * call may be captured into a graph once the library is initialised on the
+ * device.  A captured call keeps its numbers (steps, rates, sizes) and its
+ * pointers, and everything it reads it reads at every replay.
+ *
+ * Arithmetic is fp32 (64 bits where said), whatever the elements' types;
+ * every result is rounded once, to nearest even.  Each sum has an order that
+ * goes by the sizes alone: the same inputs give the same bits for every
+ * workgroup budget.  workgroups_per_step is the most workgroups of a launch
+ * (0: as many as there is work for); threads_per_workgroup does not apply.
+ * Statistics as for a collective, every launch counted in reduce_launches.
+ *
+ * Pointers are device pointers aligned to their elements (any further
+ * alignment is taken; buffers that start on a 128-byte line are the fastest).
+ * What a call writes may overlap nothing else of the call but where an
+ * operator says so; HOCCL_ERR_INVALID_ARG otherwise.
+ *
+ * 8 bits.  Where values are held in 8 bits they are e4m3 (OCP: 448 at most,
+ * subnormals down to 2^-9, NaN but no infinity), and each HOCCL_BLOCK
+ * consecutive ones share an fp32 scale: value = e4m3 * scale, scale = the
+ * block's largest magnitude / 448.  A block whose largest magnitude is under
+ * 2^-100 is held as zeros with the scale 0; one that holds an infinity or a
+ * NaN reads back as NaN throughout. */
+#define HOCCL_BLOCK 128
+
+/* One tensor of an AdamW step: n elements of each (HOCCL_BLOCK-blocks start
+ * at its first).  The scales, ceil(n / HOCCL_BLOCK) of each, are for 8-bit
+ * states.  `copy` may be NULL. */
+typedef struct {
+    void *param;             /* fp32 or bf16, updated                         */
+    const void *grad;        /* fp32 or bf16                                  */
+    void *exp_avg;           /* fp32, or e4m3 bytes, updated                  */
+    void *exp_avg_sq;        /* fp32, or e4m3 bytes that hold its root        */
+    float *exp_avg_scale;
+    float *exp_avg_sq_scale;
+    void *copy;              /* bf16: receives the new parameter              */
+    size_t n;
+} hoccl_adamw_tensor_t;
+
+typedef struct {
+    hoccl_dtype_t param_dtype, grad_dtype;  /* HOCCL_FP32 or HOCCL_BF16       */
+    int state_bits;          /* 32: fp32 states; 8                            */
+    long long step;          /* this step's number, from 1                    */
+    double lr, beta1, beta2, eps, weight_decay;
+    const float *lr_dev;     /* or NULL: read instead of lr when the call runs */
+    const int32_t *step_dev; /* or NULL: read instead of step; under 1 is 1.
+                                With both a captured step can go on counting  */
+    const float *grad_scale; /* or NULL: multiplies every gradient (the
+                                coefficient of a clipped norm, a loss scale's
+                                inverse)                                      */
+} hoccl_adamw_t;
+
+/* One AdamW step over `count` tensors (a host array, read during the call):
+ *   g  = grad * grad_scale
+ *   m' = beta1 m + (1 - beta1) g,   v' = beta2 v + (1 - beta2) g g
+ *   p' = (1 - lr weight_decay) p
+ *        - lr / (1 - beta1^step) * m' / (sqrt(v' / (1 - beta2^step)) + eps)
+ * in place.  8-bit states hold m' and the root of v', rounded after the
+ * update has used them; a root that is not zero is held as 2^-9 of the scale
+ * at least, never as zero.  A rounding to 8 bits loses changes of less than
+ * half a step, 1/16 of a value: with beta2 near 1 a v that is a block's
+ * largest follows its gradients, the others follow in such steps.  bf16
+ * parameters are rounded likewise (2^-9): small updates need fp32
+ * parameters, whose bf16 `copy` is then what the all-gather sends.  Tensors
+ * of no elements are skipped; 48 tensors share a launch. */
+hoccl_status_t hoccl_adamw(const hoccl_adamw_tensor_t *tensors, int count, const hoccl_adamw_t *options,
+                           hipStream_t stream);
+
+/* Residual addition and RMS norm of `rows` rows of `hidden` (1 to 32768)
+ * elements of `dtype` (fp32 or bf16), back to back:
+ *   h = x + residual, rounded to dtype (h = x where residual is NULL)
+ *   y = h * weight / sqrt(mean(h * h) + eps)
+ * residual_out (or NULL) receives h.  y is of dtype; with `scale` it is e4m3
+ * bytes, ceil(hidden / HOCCL_BLOCK) scales a row, the last block of a row
+ * short where hidden is not a multiple: bytes an all-gather moves as
+ * HOCCL_UINT8.  residual_out, and a y of dtype, may be x or residual itself
+ * (but not both the same). */
+hoccl_status_t hoccl_rmsnorm(const void *x, const void *residual, const void *weight, void *residual_out, void *y,
+                             float *scale, size_t rows, size_t hidden, double eps, hoccl_dtype_t dtype,
+                             hoccl_dtype_t weight_dtype, hipStream_t stream);
+
+/* Its gradients.  From dy, the gradient of y (for a y in 8 bits too, whose
+ * rounding counts as none), and dresidual, the gradient of residual_out (or
+ * NULL: none), at the h of the forward call:
+ *   r = 1 / sqrt(mean(h * h) + eps)
+ *   dx = r dy weight - h r^3 mean(dy weight h) + dresidual
+ *   dweight = sum over the rows of dy h r                       (fp32)
+ * dx is the gradient of x and of the residual; it may be dy, dresidual or h
+ * itself.  dweight may be NULL; otherwise the call needs a workspace of
+ * hoccl_rmsnorm_backward_workspace bytes (4-byte aligned), whose contents
+ * before and after do not matter. */
+hoccl_status_t hoccl_rmsnorm_backward_workspace(size_t rows, size_t hidden, hoccl_dtype_t dtype, size_t *bytes);
+hoccl_status_t hoccl_rmsnorm_backward(const void *dy, const void *dresidual, const void *h, const void *weight,
+                                      void *dx, float *dweight, void *workspace, size_t workspace_bytes, size_t rows,
+                                      size_t hidden, double eps, hoccl_dtype_t dtype, hoccl_dtype_t weight_dtype,
+                                      hipStream_t stream);
+
+/* The router's balance loss.  A batch (a rank's tokens, or a sequence) has
+ * logits [tokens][experts] and choices [tokens][topk], integers; a choice
+ * outside [0, experts) is none, and a token without a choice is padding: it
+ * is in no sum and its gradient is zero, whatever its logits hold.  With T the
+ * other tokens, p = softmax(logits) of a token (0 where all its logits are
+ * -inf), n_i the choices of expert i, `ranks` ranks of experts / ranks
+ * consecutive experts each, s_d the tokens that chose an expert of rank d:
+ *   f_i = n_i experts / (topk T),   P_i = mean of p_i over the T tokens
+ *   w_i = expert_weight f_i + rank_weight (mean of f over i's rank)
+ *         + traffic_weight s_d(i) ranks / (max_ranks T)
+ *   loss = sum over i of w_i P_i
+ * (a batch without a token: 0).  n and s are counts and carry no gradient. */
+typedef struct {
+    hoccl_dtype_t logits_dtype;  /* HOCCL_FP32 or HOCCL_BF16                  */
+    int index_bytes;             /* 4 or 8: the choices' type                 */
+    int experts;                 /* 1 to 1024                                 */
+    int topk;                    /* 1 to 64                                   */
+    int ranks;                   /* 1 to 64, a divisor of experts             */
+    int max_ranks;               /* ranks a token may go to; 0: the smaller of
+                                    topk and ranks                            */
+    double expert_weight, rank_weight, traffic_weight;
+} hoccl_balance_t;
+
+/* `batches` (1 to 64) batches at once: `logits` and `choices` are host arrays
+ * of device pointers, `tokens` a host array (fewer than 2^31 / topk each).
+ * Receives, a batch each: loss (fp32), expert_tokens [experts] = n and
+ * rank_tokens [ranks] = s (int32; with a batch a rank, row r of rank_tokens
+ * times the elements of a token is row r of the dispatch's all-to-all(v)
+ * counts), and coef [experts] (fp32), (w_i - mean of w) / T, for the
+ * backward call.  The workspace: hoccl_balance_workspace bytes, 4-byte
+ * aligned, whose contents before and after do not matter. */
+hoccl_status_t hoccl_balance_workspace(const size_t *tokens, int batches, const hoccl_balance_t *options,
+                                       size_t *bytes);
+hoccl_status_t hoccl_balance_loss(const void *const *logits, const void *const *choices, const size_t *tokens,
+                                  int batches, const hoccl_balance_t *options, float *loss, int32_t *expert_tokens,
+                                  int32_t *rank_tokens, float *coef, void *workspace, size_t workspace_bytes,
+                                  hipStream_t stream);
+
+/* dlogits[b][t][j] = dloss[b] p_j (coef_j - sum over i of coef_i p_i), in the
+ * type of the logits; dloss (fp32, one a batch) may be NULL: ones. */
+hoccl_status_t hoccl_balance_loss_backward(const void *const *logits, const void *const *choices,
+                                           const size_t *tokens, int batches, const hoccl_balance_t *options,
+                                           const float *coef, const float *dloss, void *const *dlogits,
+                                           hipStream_t stream);
+
 /* ---- several processes on one device ------------------------------------
  * The paper's runtime IPC-handle exchange (Zero-SM Point-to-Point Executor,
  * intra-node communication): a process exports the allocation holding one

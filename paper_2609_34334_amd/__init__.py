@@ -9,6 +9,8 @@ C ABI declared in ``include/hoccl.h``.
 Importing fails loudly when the library has not been built: there is no
 fallback implementation.
 """
+import collections
+import contextlib
 import ctypes
 import os
 import threading
@@ -76,7 +78,35 @@ class Stats(ctypes.Structure):
                 ("copy_bytes", ctypes.c_ulonglong)]
 
 
+class _AdamW(ctypes.Structure):
+    _fields_ = [("param_dtype", ctypes.c_int),
+                ("grad_dtype", ctypes.c_int),
+                ("state_bits", ctypes.c_int),
+                ("step", ctypes.c_longlong),
+                ("lr", ctypes.c_double),
+                ("beta1", ctypes.c_double),
+                ("beta2", ctypes.c_double),
+                ("eps", ctypes.c_double),
+                ("weight_decay", ctypes.c_double),
+                ("lr_dev", ctypes.c_void_p),
+                ("step_dev", ctypes.c_void_p),
+                ("grad_scale", ctypes.c_void_p)]
+
+
+class _Balance(ctypes.Structure):
+    _fields_ = [("logits_dtype", ctypes.c_int),
+                ("index_bytes", ctypes.c_int),
+                ("experts", ctypes.c_int),
+                ("topk", ctypes.c_int),
+                ("ranks", ctypes.c_int),
+                ("max_ranks", ctypes.c_int),
+                ("expert_weight", ctypes.c_double),
+                ("rank_weight", ctypes.c_double),
+                ("traffic_weight", ctypes.c_double)]
+
+
 _vpp = ctypes.POINTER(ctypes.c_void_p)
+_vp = ctypes.c_void_p
 _sz = ctypes.c_size_t
 _szp = ctypes.POINTER(ctypes.c_size_t)
 _i = ctypes.c_int
@@ -95,6 +125,13 @@ _SIGS = {
     "hoccl_alltoall": [_vpp, _vpp, _sz, _i, _i, ctypes.c_void_p],
     "hoccl_alltoallv": [_vpp, _szp, _szp, _vpp, _szp, _i, _i, ctypes.c_void_p],
     "hoccl_ring_hop": [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, _sz, _i, _i, ctypes.c_void_p],
+    "hoccl_adamw": [_vp, _i, ctypes.POINTER(_AdamW), _vp],
+    "hoccl_rmsnorm": [_vp, _vp, _vp, _vp, _vp, _vp, _sz, _sz, ctypes.c_double, _i, _i, _vp],
+    "hoccl_rmsnorm_backward_workspace": [_sz, _sz, _i, _szp],
+    "hoccl_rmsnorm_backward": [_vp, _vp, _vp, _vp, _vp, _vp, _vp, _sz, _sz, _sz, ctypes.c_double, _i, _i, _vp],
+    "hoccl_balance_workspace": [_szp, _i, ctypes.POINTER(_Balance), _szp],
+    "hoccl_balance_loss": [_vpp, _vpp, _szp, _i, ctypes.POINTER(_Balance), _vp, _vp, _vp, _vp, _vp, _sz, _vp],
+    "hoccl_balance_loss_backward": [_vpp, _vpp, _szp, _i, ctypes.POINTER(_Balance), _vp, _vp, _vpp, _vp],
     "hoccl_debug_plan_json": [_i, _sz, _i, _i, ctypes.c_char_p, _sz, _szp],
     "hoccl_debug_schedule_json": [_i, ctypes.POINTER(ctypes.c_double), ctypes.POINTER(_i),
                                   ctypes.POINTER(_i), ctypes.c_double, ctypes.c_double,
@@ -512,4 +549,278 @@ def ring_hop(partial, local, out=None, hop="middle", stream=None):
     with torch.cuda.device(local.device):
         _check(_lib.hoccl_ring_hop(partial.data_ptr(), local.data_ptr(), out.data_ptr(), local.numel(),
                                    dt, h, _stream(stream)), "hoccl_ring_hop")
+    return out
+
+
+# ---- operators on a rank's shard (include/hoccl.h has their formulas) ---------------
+
+BLOCK = 128                     # values in 8 bits that share a scale
+_FLOATS = {torch.float32: FP32, torch.bfloat16: BF16}
+_NOWHERE = contextlib.nullcontext()
+
+
+def _at(device, stream):
+    """The context of a call on `device`: that GPU current and, given a
+    stream, the stream too, so that what the call allocates belongs to it."""
+    if device.type != "cuda":
+        raise ValueError("tensors must live on a GPU")
+    if stream is None:
+        return _NOWHERE if torch.cuda.current_device() == device.index else torch.cuda.device(device)
+    if stream.device != device:
+        raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
+    return torch.cuda.stream(stream)
+
+
+def _handle(stream):
+    return torch.cuda.current_stream().cuda_stream if stream is None else stream.cuda_stream
+
+
+def _want(t, name, device, dtypes, shape=None):
+    """Checks one operand; returns its dtype's code (or None)."""
+    if t.dtype not in dtypes:
+        raise TypeError(f"{name} must be {' or '.join(map(str, dtypes))}, not {t.dtype}")
+    if t.device != device:
+        raise ValueError("all buffers must live on the same GPU")
+    if not t.is_contiguous():
+        raise ValueError("buffers must be contiguous")
+    if shape is not None and t.shape != shape:
+        raise ValueError(f"{name} has the shape {tuple(t.shape)}, not {tuple(shape)}")
+    return _FLOATS.get(t.dtype)
+
+
+def _scalar(t, name, device, dtype):
+    if t.numel() != 1:
+        raise ValueError(f"{name} must have one element")
+    _want(t, name, device, (dtype,))
+    return t.data_ptr()
+
+
+def adamw_state(params, bits=32):
+    """(exp_avgs, exp_avg_sqs, exp_avg_scales, exp_avg_sq_scales) of a first
+    adamw step over `params`: zeros, fp32 and no scales (None), or in 8 bits
+    with the scales of each BLOCK elements."""
+    if bits not in (8, 32):
+        raise ValueError(f"bits is 8 or 32, not {bits}")
+
+    def zeros(shape_of, dtype):
+        return [torch.zeros(shape_of(p), dtype=dtype, device=p.device) for p in params]
+
+    if bits == 32:
+        return zeros(lambda p: p.shape, torch.float32), zeros(lambda p: p.shape, torch.float32), None, None
+    q = lambda: [t.view(torch.float8_e4m3fn) for t in zeros(lambda p: p.shape, torch.uint8)]
+    s = lambda: zeros(lambda p: -(-p.numel() // BLOCK), torch.float32)
+    return q(), q(), s(), s()
+
+
+def adamw(params, grads, exp_avgs, exp_avg_sqs, exp_avg_scales=None, exp_avg_sq_scales=None, *, step, lr,
+          betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, copies=None, grad_scale=None, stream=None):
+    """One AdamW step over lists of tensors, in place (hoccl_adamw).  All
+    params share a dtype (fp32 or bf16), and all grads.  The states are fp32,
+    or float8_e4m3fn with their scales (adamw_state makes either).  `copies`:
+    bf16 tensors (or None for some) that receive the new parameters.  `step`
+    counts from 1; it may be an int32 tensor of one element on the GPU and
+    `lr` an fp32 one, which are then read when the work runs.  `grad_scale`:
+    an fp32 tensor of one element that multiplies every gradient.  Returns
+    `params`."""
+    n = len(params)
+    eight = exp_avg_scales is not None
+    if eight != (exp_avg_sq_scales is not None):
+        raise ValueError("8-bit states need the scales of both")
+    lists = [("grads", grads), ("exp_avgs", exp_avgs), ("exp_avg_sqs", exp_avg_sqs)]
+    if eight:
+        lists += [("exp_avg_scales", exp_avg_scales), ("exp_avg_sq_scales", exp_avg_sq_scales)]
+    if copies is not None:
+        lists.append(("copies", copies))
+    for name, ts in lists:
+        if len(ts) != n:
+            raise ValueError(f"{name} has {len(ts)} tensors, params {n}")
+    if n == 0:
+        return params
+    device, pdt, gdt = params[0].device, params[0].dtype, grads[0].dtype
+    if pdt not in _FLOATS or gdt not in _FLOATS:
+        raise TypeError(f"params and grads must be fp32 or bf16, not {pdt} and {gdt}")
+    states = torch.float8_e4m3fn if eight else torch.float32
+    flat = []
+    for i in range(n):
+        p, shape = params[i], params[i].shape
+        row = [p, grads[i], exp_avgs[i], exp_avg_sqs[i]]
+        for t, dt, name in zip(row, (pdt, gdt, states, states), ("params", "grads", "exp_avgs", "exp_avg_sqs")):
+            if t.dtype != dt or t.device != device or t.shape != shape or not t.is_contiguous():
+                _want(t, f"{name}[{i}]", device, (dt,), shape)
+        ptrs = [t.data_ptr() for t in row]
+        if eight:
+            blocks = (-(-p.numel() // BLOCK),)
+            for t, name in ((exp_avg_scales[i], "exp_avg_scales"), (exp_avg_sq_scales[i], "exp_avg_sq_scales")):
+                _want(t, f"{name}[{i}]", device, (torch.float32,), blocks)
+                ptrs.append(t.data_ptr())
+        else:
+            ptrs += (0, 0)
+        c = None if copies is None else copies[i]
+        if c is not None:
+            _want(c, f"copies[{i}]", device, (torch.bfloat16,), shape)
+        flat += ptrs
+        flat += (0 if c is None else c.data_ptr(), p.numel())
+    with _at(device, stream):
+        o = _AdamW(_FLOATS[pdt], _FLOATS[gdt], 8 if eight else 32, 0, 0.0, betas[0], betas[1], eps, weight_decay)
+        if isinstance(step, torch.Tensor):
+            o.step_dev = _scalar(step, "step", device, torch.int32)
+        else:
+            o.step = step
+        if isinstance(lr, torch.Tensor):
+            o.lr_dev = _scalar(lr, "lr", device, torch.float32)
+        else:
+            o.lr = lr
+        if grad_scale is not None:
+            o.grad_scale = _scalar(grad_scale, "grad_scale", device, torch.float32)
+        _check(_lib.hoccl_adamw((ctypes.c_uint64 * len(flat))(*flat), n, ctypes.byref(o), _handle(stream)), "hoccl_adamw")
+    return params
+
+
+def _rows(x):
+    if x.dim() == 0:
+        raise ValueError("rows of at least one dimension are needed")
+    hidden = x.shape[-1]
+    return (x.numel() // hidden if hidden else 0), hidden
+
+
+def rmsnorm(x, weight, residual=None, *, eps=1e-6, quantize=False, out=None, residual_out=None, stream=None):
+    """RMS norm over the last dimension of x, or of h = x + residual
+    (hoccl_rmsnorm).  Returns y, and with a residual (y, h): h is the new
+    residual, rounded to the type of x.  With `quantize` y is a pair of
+    float8_e4m3fn values, shaped like x, and fp32 scales [..., blocks of
+    BLOCK].  `out` (y, or the pair) and `residual_out` default to new tensors;
+    y and residual_out may each be x or residual itself."""
+    device = x.device
+    dt = _want(x, "x", device, _FLOATS)
+    rows, hidden = _rows(x)
+    wdt = _want(weight, "weight", device, _FLOATS, (hidden,))
+    if residual is not None:
+        _want(residual, "residual", device, (x.dtype,), x.shape)
+    with _at(device, stream):
+        q = scale = y = None
+        if quantize:
+            blocks = x.shape[:-1] + (-(-hidden // BLOCK),)
+            if out is None:
+                q = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=device)
+                scale = torch.empty(blocks, dtype=torch.float32, device=device)
+            else:
+                q, scale = out
+                _want(q, "out", device, (torch.float8_e4m3fn,), x.shape)
+                _want(scale, "the scales of out", device, (torch.float32,), blocks)
+        else:
+            y = torch.empty_like(x) if out is None else out
+            if out is not None:
+                _want(y, "out", device, (x.dtype,), x.shape)
+        if residual_out is None:
+            if residual is not None:
+                residual_out = torch.empty_like(x)
+        else:
+            _want(residual_out, "residual_out", device, (x.dtype,), x.shape)
+        if rows:
+            _check(_lib.hoccl_rmsnorm(x.data_ptr(), None if residual is None else residual.data_ptr(), weight.data_ptr(),
+                                      None if residual_out is None else residual_out.data_ptr(),
+                                      (q if quantize else y).data_ptr(), scale.data_ptr() if quantize else None,
+                                      rows, hidden, eps, dt, wdt, _handle(stream)), "hoccl_rmsnorm")
+    y = (q, scale) if quantize else y
+    return y if residual is None else (y, residual_out)
+
+
+def rmsnorm_backward(grad, h, weight, grad_residual=None, *, eps=1e-6, weight_grad=True, out=None, stream=None):
+    """(dx, dweight) of rmsnorm at h (x, or the h that it returned), from the
+    gradient of y and, if any, that of h from elsewhere
+    (hoccl_rmsnorm_backward).  dx is the gradient of x and of the residual, in
+    `out` (a new tensor; or grad, grad_residual or h itself); dweight is fp32,
+    or None without `weight_grad`."""
+    device = h.device
+    dt = _want(h, "h", device, _FLOATS)
+    rows, hidden = _rows(h)
+    wdt = _want(weight, "weight", device, _FLOATS, (hidden,))
+    _want(grad, "grad", device, (h.dtype,), h.shape)
+    if grad_residual is not None:
+        _want(grad_residual, "grad_residual", device, (h.dtype,), h.shape)
+    if out is not None:
+        _want(out, "out", device, (h.dtype,), h.shape)
+    with _at(device, stream):
+        dx = torch.empty_like(h) if out is None else out
+        dweight = ws = None
+        need = ctypes.c_size_t(0)
+        if weight_grad:
+            dweight = torch.empty(hidden, dtype=torch.float32, device=device)
+            if hidden:
+                _check(_lib.hoccl_rmsnorm_backward_workspace(rows, hidden, dt, ctypes.byref(need)),
+                       "hoccl_rmsnorm_backward_workspace")
+            ws = torch.empty(need.value, dtype=torch.uint8, device=device)
+        if hidden:
+            _check(_lib.hoccl_rmsnorm_backward(grad.data_ptr(),
+                                               None if grad_residual is None else grad_residual.data_ptr(),
+                                               h.data_ptr(), weight.data_ptr(), dx.data_ptr(),
+                                               dweight.data_ptr() if weight_grad else None,
+                                               ws.data_ptr() if weight_grad else None, need.value, rows, hidden, eps,
+                                               dt, wdt, _handle(stream)), "hoccl_rmsnorm_backward")
+    return dx, dweight
+
+
+BalanceLoss = collections.namedtuple("BalanceLoss", "loss expert_tokens rank_tokens coef")
+
+
+def _balance(logits, experts, ranks, weights=(0.0, 0.0, 0.0), max_ranks=0):
+    """The options and host arrays of both directions."""
+    if not logits or len(logits) != len(experts):
+        raise ValueError("logits and experts must be lists of the same length, one tensor a batch")
+    device, dtype, index = logits[0].device, logits[0].dtype, experts[0].dtype
+    if dtype not in _FLOATS:
+        raise TypeError(f"logits must be fp32 or bf16, not {dtype}")
+    if index not in (torch.int32, torch.int64):
+        raise TypeError(f"experts must be int32 or int64, not {index}")
+    if logits[0].dim() != 2 or experts[0].dim() != 2:
+        raise ValueError("logits are [tokens, experts], experts [tokens, topk]")
+    E, k = logits[0].shape[1], experts[0].shape[1]
+    for x, e in zip(logits, experts):
+        _want(x, "logits", device, (dtype,), (x.shape[0], E))
+        _want(e, "experts", device, (index,), (x.shape[0], k))
+    n = len(logits)
+    tokens = (ctypes.c_size_t * n)(*[x.shape[0] for x in logits])
+    o = _Balance(_FLOATS[dtype], index.itemsize, E, k, ranks, max_ranks, *weights)
+    return device, o, tokens, _ptrs(logits), _ptrs(experts)
+
+
+def balance_loss(logits, experts, ranks=1, *, expert_weight=1.0, rank_weight=0.0, traffic_weight=0.0, max_ranks=None,
+                 stream=None):
+    """The router's balance loss over lists of batches, one a rank or a
+    sequence (hoccl_balance_loss): logits [tokens, E] (fp32 or bf16), experts
+    [tokens, topk] (int32 or int64; what is outside [0, E) is no choice, a
+    token without a choice is padding), `ranks` ranks of E / ranks experts.
+    Returns a BalanceLoss: loss [batches], expert_tokens [batches, E] and
+    rank_tokens [batches, ranks] (int32: choices of an expert, tokens sent to
+    a rank), and coef, which balance_loss_backward takes."""
+    device, o, tokens, lp, ep = _balance(logits, experts, ranks, (expert_weight, rank_weight, traffic_weight),
+                                         0 if max_ranks is None else max_ranks)
+    n = len(logits)
+    with _at(device, stream):
+        need = ctypes.c_size_t(0)
+        _check(_lib.hoccl_balance_workspace(tokens, n, ctypes.byref(o), ctypes.byref(need)), "hoccl_balance_workspace")
+        ws = torch.empty(need.value, dtype=torch.uint8, device=device)
+        loss = torch.empty(n, dtype=torch.float32, device=device)
+        counts = torch.empty(n, o.experts, dtype=torch.int32, device=device)
+        sent = torch.empty(n, ranks, dtype=torch.int32, device=device)
+        coef = torch.empty(n, o.experts, dtype=torch.float32, device=device)
+        _check(_lib.hoccl_balance_loss(lp, ep, tokens, n, ctypes.byref(o), loss.data_ptr(), counts.data_ptr(),
+                                       sent.data_ptr(), coef.data_ptr(), ws.data_ptr(), need.value, _handle(stream)),
+               "hoccl_balance_loss")
+    return BalanceLoss(loss, counts, sent, coef)
+
+
+def balance_loss_backward(logits, experts, coef, grad=None, *, stream=None):
+    """The gradients of the logits, from balance_loss's coef and the gradient
+    of its losses (fp32 [batches]; ones by default)."""
+    device, o, tokens, lp, ep = _balance(logits, experts, 1)
+    n = len(logits)
+    _want(coef, "coef", device, (torch.float32,), (n, o.experts))
+    if grad is not None:
+        _want(grad, "grad", device, (torch.float32,), (n,))
+    with _at(device, stream):
+        out = [torch.empty_like(x) for x in logits]
+        _check(_lib.hoccl_balance_loss_backward(lp, ep, tokens, n, ctypes.byref(o), coef.data_ptr(),
+                                                None if grad is None else grad.data_ptr(), _ptrs(out),
+                                                _handle(stream)), "hoccl_balance_loss_backward")
     return out

@@ -1,0 +1,176 @@
+// AdamW over many tensors in one launch, states in 32 or 8 bits.
+//
+//   g  = grad * grad_scale
+//   m' = beta1 m + (1 - beta1) g        v' = beta2 v + (1 - beta2) g g
+//   p' = (1 - lr wd) p - lr / (1 - beta1^t) m' / (sqrt(v') / sqrt(1 - beta2^t) + eps)
+//
+// and, where a copy is asked for, bf16(p'): what the all-gather of the
+// parameters sends out.  All arithmetic is in fp32, whatever is stored.
+//
+// 8-bit states: a block of 128 elements of a tensor keeps m' as e4m3 values
+// and their fp32 scale (largest magnitude over 448), and v' as sqrt(v') in
+// the same form, which halves the range that v' spans.  m' and v' are
+// rounded only after the update has used them.  A root that is not zero is
+// never stored as zero (2^-9 of the scale at least): the next step divides
+// by it.
+//
+// The states' products and sums are written without fused multiply-adds,
+// and sqrt and the scales' divisions are correctly rounded, so that the
+// states are those of the formulas taken one operation at a time in fp32.
+//
+// Bound by memory: 28 bytes an element (fp32 parameters and states, bf16
+// gradients and copies), 16.1 with 8-bit states.
+#include <algorithm>
+
+#include "lanes.h"
+#include "shard_ops.h"
+
+#pragma clang fp contract(off)
+
+namespace hoccl {
+namespace {
+
+constexpr int kVE = 4;  // elements of a lane's vector: 32 lanes hold a block
+template <bool Q8>
+constexpr int kU = 2;   // vectors of a thread in a tile
+template <bool Q8>
+constexpr uint32_t kTile = kOpThreads * kVE * kU<Q8>;
+
+struct Hyper {
+    float b1, c1, b2, c2, decay, rate, root, eps, gs;
+};
+
+// New moments of one element, and its parameter.
+__device__ __forceinline__ float step_one(const Hyper &h, float p, float g, float &m, float &v, float &r) {
+    g = g * h.gs;
+    m = m * h.b1 + g * h.c1;
+    v = v * h.b2 + g * g * h.c2;
+    r = __builtin_sqrtf(v);
+    return p * h.decay - h.rate * m / (r * h.root + h.eps);
+}
+
+// One block's 128 values, kVE in each of 32 lanes, as e4m3 bytes and a scale.
+template <bool FLOOR>
+__device__ __forceinline__ void put_block(const float (&x)[kVE], void *q, float *scale, uint64_t e, uint64_t n) {
+    const float top = __uint_as_float(join_lanes<kBlock / kVE, LaneUMax>(top_bits(x)));
+    float s, inv, y[kVE];
+    block_scale(top, s, inv);
+#pragma unroll
+    for (int i = 0; i < kVE; ++i) {
+        y[i] = x[i] * inv;
+        if (FLOOR) y[i] = y[i] > 0.0f && y[i] < kLeast ? kLeast : y[i];
+    }
+    Raw<kVE> r;
+    to_e4m3(y, r);
+    store_bytes(q, e, n, r);
+    if (e % kBlock == 0 && e < n) scale[e / kBlock] = s;
+}
+
+template <class TP, class TG, bool Q8>
+__device__ __forceinline__ void tile(const AdamSeg &s, const Hyper &h, uint64_t base) {
+    constexpr int U = kU<Q8>;
+    const uint64_t n = s.n;
+    float p[U][kVE], g[U][kVE], m[U][kVE], v[U][kVE];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const uint64_t e = base + (uint64_t)(u * kOpThreads + threadIdx.x) * kVE;
+        load_some<TP>(s.param, e, n, p[u]);
+        load_some<TG>(s.grad, e, n, g[u]);
+        if constexpr (Q8) {
+            Raw<kVE> a, b;
+            load_bytes(s.m, e, n, a);
+            load_bytes(s.v, e, n, b);
+            const float sm = e < n ? s.m_scale[e / kBlock] : 0.0f, sv = e < n ? s.v_scale[e / kBlock] : 0.0f;
+            from_e4m3(a, m[u]);
+            from_e4m3(b, v[u]);
+#pragma unroll
+            for (int i = 0; i < kVE; ++i) {
+                m[u][i] *= sm;
+                const float r = v[u][i] * sv;
+                v[u][i] = r * r;
+            }
+        } else {
+            load_some<EF32>(s.m, e, n, m[u]);
+            load_some<EF32>(s.v, e, n, v[u]);
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const uint64_t e = base + (uint64_t)(u * kOpThreads + threadIdx.x) * kVE;
+        float r[kVE];
+#pragma unroll
+        for (int i = 0; i < kVE; ++i) p[u][i] = step_one(h, p[u][i], g[u][i], m[u][i], v[u][i], r[i]);
+        if constexpr (Q8) {
+            // Behind the end everything is zero but an undefined 0 / 0.
+            put_block<false>(m[u], s.m, s.m_scale, e, n);
+            put_block<true>(r, s.v, s.v_scale, e, n);
+        } else {
+            store_some<EF32>(s.m, e, n, m[u]);
+            store_some<EF32>(s.v, e, n, v[u]);
+        }
+        store_some<TP>(s.param, e, n, p[u]);
+        if (s.copy) store_some<EBF16>(s.copy, e, n, p[u]);
+    }
+}
+
+template <class TP, class TG, bool Q8, int CAP>
+__global__ void __launch_bounds__(kOpThreads) adamw_kernel(AdamArgsT<CAP>) {
+    const AdamArgsT<CAP> &a = kernel_args<AdamArgsT<CAP>>();
+    const AdamStep &c = a.step;
+    Hyper h = {c.b1, c.c1, c.b2, c.c2, c.decay, c.rate, c.root, c.eps, c.grad_scale ? *c.grad_scale : 1.0f};
+    if (c.lr_dev || c.t_dev) {
+        // 1 - beta^t in 64 bits: in 32 the difference of the first steps
+        // would keep four digits.
+        const double lr = c.lr_dev ? (double)*c.lr_dev : c.lr;
+        const double t = c.t_dev ? fmax(1.0, (double)*c.t_dev) : c.t;
+        h.decay = (float)(1.0 - lr * c.weight_decay);
+        h.rate = (float)(lr / -expm1(t * c.log_b1));
+        h.root = (float)(1.0 / sqrt(-expm1(t * c.log_b2)));
+    }
+    const uint32_t tiles = a.first[a.nseg];
+    for (uint32_t t = blockIdx.x; t < tiles; t += gridDim.x) {
+        int lo = 0, hi = a.nseg;
+        while (hi - lo > 1) {
+            const int mid = (lo + hi) / 2;
+            if (a.first[mid] <= t) lo = mid;
+            else hi = mid;
+        }
+        tile<TP, TG, Q8>(a.seg[lo], h, (uint64_t)(t - a.first[lo]) * kTile<Q8>);
+    }
+}
+
+template <int CAP>
+hipError_t launch(const AdamArgsT<CAP> &a, hoccl_dtype_t param, hoccl_dtype_t grad, int bits, int wg, hipStream_t s) {
+    const bool pb = param == HOCCL_BF16, gb = grad == HOCCL_BF16, q = bits == 8;
+    const void *k;
+    if (pb)
+        k = gb ? (q ? (const void *)adamw_kernel<EBF16, EBF16, true, CAP>
+                    : (const void *)adamw_kernel<EBF16, EBF16, false, CAP>)
+               : (q ? (const void *)adamw_kernel<EBF16, EF32, true, CAP>
+                    : (const void *)adamw_kernel<EBF16, EF32, false, CAP>);
+    else
+        k = gb ? (q ? (const void *)adamw_kernel<EF32, EBF16, true, CAP>
+                    : (const void *)adamw_kernel<EF32, EBF16, false, CAP>)
+               : (q ? (const void *)adamw_kernel<EF32, EF32, true, CAP>
+                    : (const void *)adamw_kernel<EF32, EF32, false, CAP>);
+    void *args[] = {(void *)&a};
+    return hipLaunchKernel(k, dim3((unsigned)wg), dim3(kOpThreads), args, 0, s);
+}
+
+}  // namespace
+
+uint32_t adamw_tile(int state_bits) { return state_bits == 8 ? kTile<true> : kTile<false>; }
+
+hipError_t launch_adamw(const AdamArgs &a, hoccl_dtype_t param, hoccl_dtype_t grad, int state_bits, int wg,
+                        hipStream_t s) {
+    if (a.nseg > kAdamFewSegs) return launch(a, param, grad, state_bits, wg, s);
+    // Few tensors pass a smaller struct, which the runtime stages faster.
+    AdamArgsT<kAdamFewSegs> f;
+    std::copy(a.seg, a.seg + a.nseg, f.seg);
+    std::copy(a.first, a.first + a.nseg + 1, f.first);
+    f.nseg = a.nseg;
+    f.step = a.step;
+    return launch(f, param, grad, state_bits, wg, s);
+}
+
+}  // namespace hoccl

@@ -30,6 +30,7 @@
 #include <string>
 #include <vector>
 
+#include "call.h"
 #include "ceilings.h"
 #include "errors.h"
 #include "hoccl_internal.h"
@@ -1101,6 +1102,68 @@ PlanOptions options_from(const hoccl_config_t &cfg, bool in_place) {
 }  // namespace
 
 void set_error_message(const char *msg) { t_err = msg; }
+
+void format_error(const char *fmt, ...) {
+    char buf[512];
+    va_list ap;
+    va_start(ap, fmt);
+    vsnprintf(buf, sizeof buf, fmt, ap);
+    va_end(ap);
+    t_err = buf;
+}
+
+// ---- operator calls (call.h) --------------------------------------------------------
+
+struct OpCall::Impl {
+    std::chrono::steady_clock::time_point t0 = std::chrono::steady_clock::now();
+    DeviceState *st = nullptr;
+    std::unique_lock<std::recursive_mutex> lock;
+    hoccl_config_t cfg;
+    hipStream_t s = nullptr;
+    TimingPair *tp = nullptr;
+};
+
+OpCall::OpCall() : impl_(new Impl) {}
+OpCall::~OpCall() = default;
+
+hoccl_status_t OpCall::open(hipStream_t s) {
+    hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+    HIP_TRY(hipStreamIsCapturing(s, &cap));
+    const bool capturing = cap != hipStreamCaptureStatusNone;
+    TRY(get_state(&impl_->st, capturing));
+    impl_->lock = std::unique_lock<std::recursive_mutex>(impl_->st->call_mu);
+    impl_->cfg = config();
+    if (capturing) impl_->cfg.kernel_timing = 0;
+    impl_->s = s;
+    std::memset(&t_stats, 0, sizeof t_stats);
+    t_stats.cus_available = impl_->st->num_cus;
+    return HOCCL_OK;
+}
+
+int OpCall::cus() const { return impl_->st->num_cus; }
+
+int OpCall::budget(unsigned long long want) const {
+    const int most = impl_->cfg.workgroups_per_step;
+    if (most > 0 && want > (unsigned long long)most) return most;
+    return (int)std::min(std::max(want, 1ull), 1ull << 30);
+}
+
+hoccl_status_t OpCall::before() { return timed_begin(*impl_->st, impl_->cfg, impl_->s, &impl_->tp); }
+
+hoccl_status_t OpCall::after(int wg, hipError_t e) {
+    HIP_TRY(e);
+    TRY(timed_end(impl_->tp, impl_->s));
+    t_stats.reduce_launches++;
+    t_stats.workgroups_per_step = std::max(t_stats.workgroups_per_step, wg);
+    t_stats.cus_used_max = std::max(t_stats.cus_used_max, std::min(wg, impl_->st->num_cus));
+    return HOCCL_OK;
+}
+
+void OpCall::done(unsigned long long hbm_bytes) {
+    t_stats.hbm_bytes_algorithmic = hbm_bytes;
+    t_stats.host_enqueue_us =
+        std::chrono::duration<double, std::micro>(std::chrono::steady_clock::now() - impl_->t0).count();
+}
 
 }  // namespace hoccl
 

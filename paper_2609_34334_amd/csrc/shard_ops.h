@@ -1,0 +1,119 @@
+// The operators that a training step runs on a rank's shard between two
+// collectives: argument structs and launchers of adamw.hip, rmsnorm.hip and
+// balance.hip.
+#pragma once
+
+#include <hip/hip_runtime_api.h>
+
+#include <cstddef>
+#include <cstdint>
+
+#include "../../include/hoccl.h"
+
+namespace hoccl {
+
+constexpr int kOpThreads = 256;  // per workgroup, of every kernel but the wide rows of rmsnorm.hip
+
+// ---- AdamW ------------------------------------------------------------------
+
+struct AdamSeg {
+    void *param;
+    const void *grad;
+    void *m, *v;
+    float *m_scale, *v_scale;
+    void *copy;
+    uint64_t n;
+};
+
+struct AdamStep {
+    float b1, c1, b2, c2;            // beta1, 1 - beta1, beta2, 1 - beta2
+    float decay, rate, root, eps;    // 1 - lr wd, lr / (1 - beta1^t), 1 / sqrt(1 - beta2^t)
+    double lr, weight_decay, log_b1, log_b2, t;  // where lr or t is on the device
+    const float *lr_dev;
+    const int32_t *t_dev;
+    const float *grad_scale;
+};
+// One launch's tensors.  first[i] is the tile at which tensor i starts.
+template <int CAP>
+struct AdamArgsT {
+    AdamSeg seg[CAP];
+    uint32_t first[CAP + 1];
+    int nseg;
+    AdamStep step;
+};
+constexpr int kAdamSegs = 48;        // 3.4 KiB of arguments
+constexpr int kAdamFewSegs = 8;
+using AdamArgs = AdamArgsT<kAdamSegs>;
+
+uint32_t adamw_tile(int state_bits);  // elements of one tile
+hipError_t launch_adamw(const AdamArgs &a, hoccl_dtype_t param, hoccl_dtype_t grad, int state_bits, int wg,
+                        hipStream_t s);
+
+// ---- RMSNorm -----------------------------------------------------------------
+
+constexpr size_t kMaxHidden = 32768;
+
+struct RmsArgs {
+    const void *x, *residual, *weight;
+    void *residual_out, *y;   // y: T, or e4m3 bytes with `scale`
+    float *scale;
+    uint64_t rows;
+    uint32_t hidden;
+    int weight_bf16;
+    float eps;
+};
+struct RmsBackArgs {
+    const void *dy, *dres, *h, *weight;
+    void *dx;
+    float *partial;           // [blocks][hidden], or null: no weight gradient
+    uint64_t rows;
+    uint32_t hidden, blocks;
+    int weight_bf16;
+    float eps;
+};
+
+// Workgroups of the automatic launch.
+unsigned long long rmsnorm_workgroups(size_t rows, size_t hidden, hoccl_dtype_t dt, int cus);
+hipError_t launch_rmsnorm(const RmsArgs &a, hoccl_dtype_t dt, int wg, hipStream_t s);
+// Partial sums of the weight's gradient: a number that goes by the sizes
+// alone, so that the result does not depend on the workgroups.
+uint32_t rmsnorm_backward_blocks(size_t rows, size_t hidden, hoccl_dtype_t dt);
+hipError_t launch_rmsnorm_backward(const RmsBackArgs &a, hoccl_dtype_t dt, int wg, hipStream_t s);
+uint32_t rmsnorm_grad_workgroups(size_t hidden);
+hipError_t launch_rmsnorm_weight_grad(const float *partial, uint32_t blocks, uint32_t hidden, float *dweight, int wg,
+                                      hipStream_t s);
+
+// ---- balance loss -------------------------------------------------------------
+
+constexpr int kMaxExperts = 1024;
+constexpr int kMaxTopk = 64;
+constexpr int kMaxBatches = 64;
+
+struct BalanceSeg {
+    const void *logits;
+    const void *experts;
+    void *dlogits;
+    uint64_t tokens;
+};
+struct BalanceArgs {
+    BalanceSeg seg[kMaxBatches];
+    uint32_t first[kMaxBatches + 1];  // first block of each batch
+    int nseg, E, k, D;
+    int index64;
+    float *partial_p;      // [blocks][E]
+    int32_t *partial_n;    // [blocks][E + D + 1]: choices, tokens a rank, tokens
+    float *loss;           // [nseg]
+    int32_t *expert_tokens, *rank_tokens;  // [nseg][E], [nseg][D]
+    float *coef;           // [nseg][E]
+    const float *grad;     // [nseg] or null
+    double expert_weight, rank_weight, traffic_weight;
+    int max_ranks;
+};
+
+uint32_t balance_blocks(size_t tokens, int E, int batches);
+hipError_t launch_balance(const BalanceArgs &a, hoccl_dtype_t dt, int wg, hipStream_t s);
+hipError_t launch_balance_finish(const BalanceArgs &a, int wg, hipStream_t s);
+uint32_t balance_backward_blocks(size_t tokens, int E);
+hipError_t launch_balance_backward(const BalanceArgs &a, hoccl_dtype_t dt, int wg, hipStream_t s);
+
+}  // namespace hoccl

@@ -1,0 +1,310 @@
+"""AdamW (hoccl_adamw) against the formulas in 64 bits.
+
+Tolerances count roundings, each at most half a step (U = 2^-24 of the value
+in fp32, 2^-8 in bf16), from the operator's own inputs.  fp32 states: m' is
+two products and a sum of rounded factors, v' likewise with the square.
+8-bit states are compared twice: bit for bit with the formulas taken one
+operation at a time in fp32 on the CPU, and with 64 bits to half a step of
+e4m3 (2^-4 of the value, 2^-10 of the scale below its normal range)."""
+import math
+
+import numpy as np
+import pytest
+import torch
+
+import paper_2609_34334_amd as hc
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+BF = 2.0 ** -8
+HYPER = dict(lr=2e-3, betas=(0.9, 0.99), eps=1e-8, weight_decay=0.1)
+
+
+@pytest.fixture(autouse=True)
+def _defaults():
+    saved = hc.get_config()
+    yield
+    hc.set_config(**saved)
+
+
+def blocks_of(x, n=128):
+    pad = -x.numel() % n
+    return torch.nn.functional.pad(x.flatten(), (0, pad)).view(-1, n)
+
+
+def dequantize(q, s):
+    return (blocks_of(q.float()) * s[:, None]).flatten()[:q.numel()]
+
+
+def quantize(x, floor):
+    """One fp32 operation at a time, on the CPU."""
+    b = blocks_of(x)
+    top = b.abs().amax(1)
+    some = ~(top < 2.0 ** -100)
+    scale = torch.where(some, top / 448.0, torch.zeros(()))
+    # a tensor over a tensor: a number over a tensor is torch's reciprocal times the number, two roundings
+    q = b * torch.where(some, torch.full_like(top, 448.0) / top, torch.zeros(()))[:, None]
+    if floor:
+        q = torch.where((q > 0) & (q < 2.0 ** -9), torch.tensor(2.0 ** -9), q)
+    return q.flatten()[:x.numel()].to(torch.float8_e4m3fn), scale
+
+
+class Case:
+    """Tensors of the sizes, cut out of flat buffers with `shift` elements
+    before each and a guard behind it."""
+
+    def __init__(self, sizes, seed, param="fp32", grad="bf16", bits=32, copy=True, shift=0, zero=0.1, fresh=False):
+        g = torch.Generator().manual_seed(seed)
+        dts = {"fp32": torch.float32, "bf16": torch.bfloat16}
+        self.sizes, self.bits, self.guards = sizes, bits, []
+        draw = lambda n: torch.randn(n, generator=g)
+        self.p, self.g, self.m, self.v, self.c = [], [], [], [], [] if copy else None
+        self.ms, self.vs = ([], []) if bits == 8 else (None, None)
+        for n in sizes:
+            level = torch.exp(2 * draw(n))
+            m, v = draw(n) * level * 0.1, level.square() * torch.rand(n, generator=g)
+            v[torch.rand(n, generator=g) < zero] = 0
+            if fresh:
+                m, v = m * 0, v * 0
+            self.p.append(self.put(draw(n).to(dts[param]), shift))
+            self.g.append(self.put((draw(n) * level).to(dts[grad]), shift))
+            if bits == 8:
+                for x, held, scales, floor in ((m, self.m, self.ms, False), (v.sqrt(), self.v, self.vs, True)):
+                    q, s = quantize(x, floor)
+                    held.append(self.put(q.view(torch.uint8), shift).view(torch.float8_e4m3fn))
+                    scales.append(self.put(s, 1))
+            else:
+                self.m.append(self.put(m, shift))
+                self.v.append(self.put(v, shift))
+            if copy:
+                self.c.append(self.put(torch.zeros(n, dtype=torch.bfloat16), shift))
+
+    def put(self, x, shift):
+        whole = torch.full((shift + len(x) + 40,), 77, dtype=x.dtype)
+        whole[shift:shift + len(x)] = x
+        whole = whole.cuda()
+        self.guards.append((whole, shift, len(x)))
+        return whole[shift:shift + len(x)]
+
+    def check_guards(self):
+        for whole, shift, n in self.guards:
+            assert (whole[:shift] == 77).all() and (whole[shift + n:] == 77).all(), "written outside a tensor"
+
+    def step(self, **kw):
+        args = dict(HYPER, step=3, copies=self.c)
+        args.update(kw)
+        return hc.adamw(self.p, self.g, self.m, self.v, self.ms, self.vs, **args)
+
+    def snapshot(self):
+        f = lambda ts: None if ts is None else [t.detach().cpu().clone() for t in ts]
+        return [f(x) for x in (self.p, self.g, self.m, self.v, self.ms, self.vs, self.c)]
+
+
+def check(case, before, step=3, scale=1.0, lr=HYPER["lr"], betas=HYPER["betas"], eps=HYPER["eps"],
+          decay=HYPER["weight_decay"]):
+    after = case.snapshot()
+    b1, b2 = betas
+    for i, n in enumerate(case.sizes):
+        p, g, m, v = (before[k][i].double() for k in range(4))
+        p1, _, m1, v1 = (after[k][i] for k in range(4))
+        if case.bits == 8:
+            m = dequantize(before[2][i], before[4][i]).double()
+            r0 = dequantize(before[3][i], before[5][i])
+            v = (r0 * r0).double()
+        g = g * scale
+        new_m, new_v = b1 * m + (1 - b1) * g, b2 * v + (1 - b2) * g * g
+        root = new_v.sqrt()
+        den = root / math.sqrt(1 - b2 ** step) + eps
+        rate = lr / (1 - b1 ** step)
+        # scale and product; beta, its product and the sum
+        err_m = 4.1 * U * (b1 * m.abs() + (1 - b1) * g.abs()) + 1e-44
+        err_v = 6.1 * U * (b2 * v + (1 - b2) * g * g) + 1e-44
+        if case.bits == 32:
+            assert ((m1.double() - new_m).abs() <= err_m).all(), f"m of tensor {i}"
+            assert ((v1.double() - new_v).abs() <= err_v).all(), f"v of tensor {i}"
+        else:
+            one = torch.float32
+            gs = before[1][i].to(one) * torch.tensor(scale, dtype=one)
+            fm = m.to(one) * np.float32(b1) + gs * np.float32(1 - b1)
+            # numpy's root, which is correctly rounded; torch's on the CPU is not always
+            fr = torch.from_numpy(np.sqrt((v.to(one) * np.float32(b2) + gs * gs * np.float32(1 - b2)).numpy()))
+            for held, scales, x, exact, floor in ((m1, after[4][i], fm, new_m, 0.0), (v1, after[5][i], fr, root, 1.0)):
+                q, s = quantize(x, floor > 0)
+                assert torch.equal(scales, s), f"scales of tensor {i}"
+                assert torch.equal(held.view(torch.uint8), q.view(torch.uint8)), f"codes of tensor {i}"
+                each = scales.double().repeat_interleave(128)[:n]
+                far = (held.double() * each - exact).abs()
+                # half a step; what the floor lifts moves by 2^-9 at most; the fp32 roundings before it
+                least = 2.0 ** -10 + floor * 2.0 ** -9
+                assert (far <= 2.0 ** -4 * exact.abs() + least * each + 20 * U * exact.abs()
+                        + (0 if floor else 1) * err_m + 1e-30).all(), f"values of tensor {i}"
+                if floor:
+                    assert ((held.double() > 0) | (exact < 1e-22) | (each == 0)).all(), "a root was lost"
+        u = rate * new_m / den
+        new_p = p * (1 - lr * decay) - u
+        # the root's error is half of v's, in all 11 roundings of the update; m's error goes through
+        err_p = 3.1 * U * p.abs() + 11.5 * U * u.abs() + rate * err_m / den + 1e-30
+        got = p1.double()
+        half = BF * (new_p.abs() + err_p) if p1.dtype == torch.bfloat16 else 0
+        assert ((got - new_p).abs() <= err_p + half).all(), f"param of tensor {i}"
+        if case.c is not None:
+            if p1.dtype == torch.float32:
+                assert torch.equal(after[6][i].view(torch.int16), p1.bfloat16().view(torch.int16)), f"copy {i}"
+            else:
+                assert torch.equal(after[6][i].view(torch.int16), p1.view(torch.int16)), f"copy {i}"
+    case.check_guards()
+
+
+SIZES = [1, 2, 3, 5, 127, 128, 129, 1000, 2047, 2048, 2049, 10007]
+
+
+@pytest.mark.parametrize("shift", [0, 1])
+@pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("grad", ["fp32", "bf16"])
+@pytest.mark.parametrize("param", ["fp32", "bf16"])
+def test_formulas(param, grad, bits, shift):
+    c = Case(SIZES, 11 + shift, param, grad, bits, copy=param == "fp32", shift=shift)
+    before = c.snapshot()
+    assert c.step() is c.p
+    torch.cuda.synchronize()
+    check(c, before)
+    s = hc.last_stats()
+    assert s["reduce_launches"] == 1 and s["copy_ops"] == 0
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_from_the_first_step_on(bits):
+    """Steps 1, 2, 3 from zero states, the gradients scaled on the device."""
+    c = Case([4100, 77], 5, bits=bits, fresh=True)
+    for step in (1, 2, 3):
+        before = c.snapshot()
+        c.step(step=step, grad_scale=torch.tensor([0.37], device="cuda"))
+        torch.cuda.synchronize()
+        check(c, before, step=step, scale=float(np.float32(0.37)))
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_extremes_of_the_numbers(bits):
+    kw = dict(lr=0.0, betas=(0.0, 0.0), eps=1e-3, weight_decay=0.0)
+    c = Case([300], 6, bits=bits)
+    before = c.snapshot()
+    c.step(step=1, **kw)
+    torch.cuda.synchronize()
+    check(c, before, 1, lr=0.0, betas=(0.0, 0.0), eps=1e-3, decay=0.0)
+    c = Case([300], 7, bits=bits)
+    before = c.snapshot()
+    c.step(step=10 ** 9)
+    torch.cuda.synchronize()
+    check(c, before, 10 ** 9)
+
+
+@pytest.mark.parametrize("count", [8, 9, 48, 49, 130])
+def test_many_tensors(count):
+    """More tensors than a launch takes, empty ones among them."""
+    sizes = [(37 * i * i + 11 * i) % 3001 for i in range(count)]
+    assert sizes[0] == 0
+    c = Case(sizes, 21, bits=8 if count % 2 else 32)
+    before = c.snapshot()
+    c.step()
+    torch.cuda.synchronize()
+    check(c, before)
+    live = sum(n > 0 for n in sizes)
+    assert hc.last_stats()["reduce_launches"] == -(-live // 48)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_budgets_and_streams_give_the_same_bits(bits):
+    runs = []
+    for wg, own_stream in ((0, False), (1, False), (3, True), (0, True)):
+        hc.set_config(workgroups_per_step=wg)
+        c = Case([5000, 70001], 31, bits=bits)
+        stream = torch.cuda.Stream() if own_stream else None
+        torch.cuda.synchronize()
+        c.step(stream=stream)
+        torch.cuda.synchronize()
+        assert wg == 0 or hc.last_stats()["workgroups_per_step"] == wg
+        runs.append(c.snapshot())
+    for r in runs[1:]:
+        for x, y in zip(runs[0], r):
+            for s, t in zip(x or [], y or []):
+                assert torch.equal(s.view(torch.uint8), t.view(torch.uint8))
+
+
+def test_numbers_on_the_device_and_replays():
+    """A captured step whose lr and step are read at every replay, against
+    eager steps of the same numbers."""
+    for bits in (32, 8):
+        a, b = Case([3000, 130], 41, bits=bits), Case([3000, 130], 41, bits=bits)
+        step = torch.ones(1, dtype=torch.int32, device="cuda")
+        lr = torch.tensor([1e-3], device="cuda")
+        warm = Case([10], 1, bits=bits)
+        warm.step()
+        torch.cuda.synchronize()
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            a.step(step=step, lr=lr)
+        for k in range(1, 4):
+            rate = 1e-3 / k
+            step.fill_(k)
+            lr.fill_(rate)
+            before = b.snapshot()
+            graph.replay()
+            torch.cuda.synchronize()
+            b.step(step=torch.tensor([k], dtype=torch.int32, device="cuda"), lr=float(np.float32(rate)))
+            torch.cuda.synchronize()
+            for x, y in zip(a.snapshot(), b.snapshot()):
+                for s, t in zip(x or [], y or []):
+                    assert torch.equal(s.view(torch.uint8), t.view(torch.uint8)), (bits, k)
+            check(b, before, step=k, lr=float(np.float32(rate)))
+        del graph
+
+
+def test_what_is_not_finite():
+    """An infinite or NaN gradient spoils its element alone with fp32 states
+    and its block of 128 with 8-bit ones."""
+    for bits in (32, 8):
+        for bad in (math.inf, -math.inf, math.nan):
+            c = Case([400], 51, bits=bits, grad="fp32")
+            c.g[0][200] = bad
+            c.step()
+            torch.cuda.synchronize()
+            p = c.p[0].cpu()
+            assert not torch.isfinite(p[200]) and torch.isfinite(torch.cat([p[:200], p[201:]])).all()
+            m = c.m[0].cpu() if bits == 32 else dequantize(c.m[0].cpu(), c.ms[0].cpu())
+            v = c.v[0].cpu() if bits == 32 else dequantize(c.v[0].cpu(), c.vs[0].cpu())
+            spoilt = torch.zeros(400, dtype=torch.bool)
+            spoilt[slice(200, 201) if bits == 32 else slice(128, 256)] = True
+            assert torch.equal(~torch.isfinite(m), spoilt) and torch.equal(~torch.isfinite(v), spoilt)
+
+
+def test_tiny_and_huge_gradients():
+    """Blocks whose magnitudes reach from under 2^-100 to 2^60."""
+    for bits in (32, 8):
+        c = Case([128 * 6], 61, grad="fp32", bits=bits, fresh=True)
+        for k, e in enumerate((-140, -110, -60, 0, 30, 60)):
+            c.g[0][128 * k:128 * (k + 1)] = c.g[0][128 * k:128 * (k + 1)].sign() * 2.0 ** e
+        before = c.snapshot()
+        c.step(step=1)
+        torch.cuda.synchronize()
+        check(c, before, step=1)
+
+
+def test_more_than_2_to_the_32_bytes():
+    """Offsets past 32 bits: one bf16 tensor of 2.2 G elements with 8-bit
+    states, looked at in places."""
+    n = (1 << 31) + 128 * 700001 + 5
+    p = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    g = torch.zeros(n, dtype=torch.bfloat16, device="cuda")
+    m, v, ms, vs = hc.adamw_state([p], bits=8)
+    at = [0, 1, 127, 128, (1 << 31) - 1, 1 << 31, (1 << 31) + 1, n - 129, n - 2, n - 1]
+    idx = torch.tensor(at, device="cuda")
+    g[idx] = torch.arange(1, len(at) + 1, device="cuda").to(torch.bfloat16)
+    hc.adamw([p], [g], m, v, ms, vs, step=1, lr=0.5, weight_decay=0.0)
+    torch.cuda.synchronize()
+    # The first step moves each parameter with a gradient by lr, the others not.
+    assert torch.allclose(p[idx].float(), torch.full((len(at),), -0.5, device="cuda"), atol=0.5 * BF * 1.01)
+    assert int((p != 0).sum()) == len(at)
+    assert int((m[0].view(torch.uint8) != 0).sum()) == len(at) == int((v[0].view(torch.uint8) != 0).sum())
+    lit = torch.unique(idx // 128)
+    assert torch.equal(torch.nonzero(ms[0]).flatten(), lit) and torch.equal(torch.nonzero(vs[0]).flatten(), lit)

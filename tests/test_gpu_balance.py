@@ -1,0 +1,282 @@
+"""The router's balance loss (hoccl_balance_loss), its counts and its gradient
+against the formulas in 64 bits.
+
+Counts are exact.  Tolerances count roundings (U = 2^-24): an exponent of a
+span of logits has three of that span (the difference, the product with
+log2 e, and that constant), exp2 two, the sum of a token's at most 16 + 6
+additions and the quotient and product three; EPS is their sum for the span
+of the test's logits."""
+import ctypes
+import math
+
+import pytest
+import torch
+
+import paper_2609_34334_amd as hc
+
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+WEIGHTS = dict(expert_weight=0.3, rank_weight=0.05, traffic_weight=0.7)
+
+
+@pytest.fixture(autouse=True)
+def _defaults():
+    saved = hc.get_config()
+    yield
+    hc.set_config(**saved)
+
+
+def batch(seed, T, E, k, dt=torch.float32, index=torch.int64, padding=0.0, span=3.0):
+    g = torch.Generator(device="cuda").manual_seed(seed)
+    x = (torch.randn(T, E, generator=g, device="cuda") + 0.5 * torch.randn(E, generator=g, device="cuda")) * span
+    e = torch.randint(0, E, (T, k), generator=g, device="cuda") if k > E else x.topk(k, -1).indices
+    e = e.to(index)
+    if padding:
+        e[torch.rand(T, generator=g, device="cuda") < padding] = -1
+        e[torch.rand(T, generator=g, device="cuda") < padding, -1] = E + 3      # no expert either
+    return x.to(dt), e
+
+
+def reference(x, e, D, expert_weight, rank_weight, traffic_weight, max_ranks=None):
+    T, E = x.shape
+    k = e.shape[1]
+    e = e.long().cpu()
+    z = x.double().cpu()
+    chosen = torch.zeros(T, E, dtype=torch.float64)
+    for c in range(k):
+        ok = (e[:, c] >= 0) & (e[:, c] < E)
+        rows = torch.nonzero(ok).flatten()
+        chosen[rows, e[rows, c]] += 1
+    live = chosen.sum(1) > 0
+    n = int(live.sum())
+    top = z.amax(1, keepdim=True)
+    ex = (z - torch.where(torch.isinf(top) & (top < 0), 0.0, top)).exp()
+    sum_ = ex.sum(1, keepdim=True)
+    p = torch.where(sum_ == 0, 0.0, ex / sum_)
+    p = torch.where(live[:, None], p, 0.0)
+    counts = chosen.sum(0)
+    sent = (chosen.view(T, D, E // D).sum(2) > 0).sum(0)
+    t = max(n, 1)
+    f = counts * E / (k * t)
+    w = (expert_weight * f + rank_weight * f.view(D, -1).mean(1).repeat_interleave(E // D)
+         + traffic_weight * (sent.double() * D / ((max_ranks or min(k, D)) * t)).repeat_interleave(E // D))
+    loss = (w * p.sum(0)).sum() / t
+    coef = (w - w.mean()) / t if n else torch.zeros(E, dtype=torch.float64)
+    return dict(loss=loss, counts=counts.int(), sent=sent.int(), coef=coef, p=p, live=live)
+
+
+def eps_of(x):
+    # A row of -inf alone has no span (its p is 0); logits over 100 below the row's largest weigh less than 2^-144.
+    span = torch.nan_to_num((x.double().amax(-1) - x.double().amin(-1)), nan=0.0).clamp(max=100.0)
+    return (3 * (float(span.max()) if x.numel() else 0.0) + 2 + 22 + 3) * U
+
+
+def check(xs, es, D, out, grads=None, g=None, max_ranks=None, **weights):
+    weights = weights or WEIGHTS
+    for b, (x, e) in enumerate(zip(xs, es)):
+        r = reference(x, e, D, max_ranks=max_ranks, **weights)
+        assert torch.equal(out.expert_tokens[b].cpu(), r["counts"]), f"expert counts of batch {b}"
+        assert torch.equal(out.rank_tokens[b].cpu(), r["sent"]), f"rank counts of batch {b}"
+        T, E = x.shape
+        eps = eps_of(x)
+        # positive terms: a token's error, the additions of a lane (tokens over workgroups and rows at most), lanes, waves
+        adds = -(-T // 1) if T < 512 else T // 64
+        scale = sum(abs(v) for v in weights.values())
+        assert abs(out.loss[b].double().cpu() - r["loss"]) <= (eps + (adds + 10) * U) * abs(r["loss"]) + 1e-30 * scale
+        # made in 64 bits, rounded once
+        assert ((out.coef[b].double().cpu() - r["coef"]).abs() <= U * r["coef"].abs() + 1e-13 * scale).all()
+        if grads is None:
+            continue
+        d = grads[b].double().cpu()
+        up = 1.0 if g is None else float(g[b])
+        p, c = r["p"], r["coef"]
+        dot = (p * c).sum(1, keepdim=True)
+        want = up * p * (c - dot)
+        around = (p * c.abs()).sum(1, keepdim=True)
+        err = abs(up) * p * ((eps + 4 * U) * (c - dot).abs() + U * c.abs() + (2 * eps + 24 * U) * around) + 1e-38
+        half = 2.0 ** -8 if x.dtype == torch.bfloat16 else U
+        assert ((d - want).abs() <= err + half * (want.abs() + err) + 1e-38).all(), f"gradient of batch {b}"
+        assert (d[~r["live"]] == 0).all()
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("E,k,D", [(1, 1, 1), (2, 1, 2), (3, 2, 3), (4, 5, 1), (8, 2, 8), (13, 4, 1), (20, 7, 10), (33, 3, 11),
+                                   (64, 6, 8), (64, 8, 64), (100, 10, 50), (129, 2, 3), (160, 6, 8), (256, 8, 64),
+                                   (260, 64, 52), (512, 8, 16), (513, 5, 27), (1023, 3, 11), (1024, 16, 64)])
+def test_formulas(E, k, D, dt):
+    xs, es = [], []
+    for i, (T, padding) in enumerate(((1, 0.0), (67, 0.0), (300, 0.3), (0, 0.0), (41, 1.1))):
+        x, e = batch(E + i, T, E, k, dt, torch.int64 if i % 2 else torch.int64, padding)
+        xs.append(x)
+        es.append(e)
+    for index in (torch.int64, torch.int32):
+        ee = [e.to(index) for e in es]
+        out = hc.balance_loss(xs, ee, D, **WEIGHTS)
+        g = torch.tensor([0.5, -2.0, 1.25, 3.0, 7.0], device="cuda")
+        grads = hc.balance_loss_backward(xs, ee, out.coef, g)
+        check(xs, ee, D, out, grads, g)
+        assert hc.last_stats()["reduce_launches"] == 1
+
+
+def test_loss_without_a_gradient_is_ones_and_weights_are_separate():
+    xs, es = zip(*[batch(5, 200, 32, 4), batch(6, 77, 32, 4)])
+    xs, es = list(xs), list(es)
+    for name in WEIGHTS:
+        w = {n: (1.5 if n == name else 0.0) for n in WEIGHTS}
+        out = hc.balance_loss(xs, es, 8, **w)
+        check(xs, es, 8, out, hc.balance_loss_backward(xs, es, out.coef), **w)
+    out = hc.balance_loss(xs, es, 8, max_ranks=3, **WEIGHTS)
+    check(xs, es, 8, out, max_ranks=3)
+
+
+@pytest.mark.parametrize("T,E,R", [(40_000, 64, 1), (20_000, 200, 3), (3_000, 64, 64), (9_000, 1024, 2)])
+def test_many_tokens(T, E, R):
+    xs, es = [], []
+    for b in range(R):
+        x, e = batch(50 + b, T - 7 * b, E, 6, torch.bfloat16 if b % 2 == 0 and R > 1 else torch.bfloat16, torch.int32, 0.1)
+        xs.append(x)
+        es.append(e)
+    out = hc.balance_loss(xs, es, 8, **WEIGHTS)
+    check(xs, es, 8, out, hc.balance_loss_backward(xs, es, out.coef))
+
+
+def test_gradient_against_differences():
+    """Central differences of the loss in 64 bits, the counts held."""
+    x, e = batch(3, 40, 24, 3, padding=0.2, span=1.0)
+    out = hc.balance_loss([x], [e], 4, **WEIGHTS)
+    (d,) = hc.balance_loss_backward([x], [e], out.coef)
+    r = reference(x, e, 4, **WEIGHTS)
+    c, live = r["coef"].cuda(), r["live"].cuda()
+
+    def f(z):   # the mean of w taken off: a constant more or less, as p sums to one
+        return (torch.softmax(z, -1)[live] * c).sum()
+
+    g = torch.Generator(device="cuda").manual_seed(1)
+    for _ in range(4):
+        u = torch.randn(x.shape, generator=g, device="cuda", dtype=torch.float64)
+        h = 1e-5
+        num = (f(x.double() + h * u) - f(x.double() - h * u)) / (2 * h)
+        ana = (d.double() * u).sum()
+        assert abs(num - ana) <= (1e-8 + 4 * eps_of(x)) * (d.double() * u).abs().sum() + 1e-12
+
+
+def test_masked_experts_and_padding_that_holds_anything():
+    """-inf and the types' lowest values among the logits; NaN, inf and
+    all -inf rows; the same in padding, where none of it shows."""
+    for dt in (torch.float32, torch.bfloat16):
+        x, e = batch(9, 60, 16, 2, dt)
+        low = torch.finfo(dt).min
+        x[3, 5] = -math.inf
+        x[4, 2:9] = low
+        x[5] = low
+        x[6] = -math.inf
+        x[7, :15] = -math.inf
+        x[8] = torch.finfo(dt).max
+        x[9, 0], x[9, 1:] = torch.finfo(dt).max, low
+        for t, bad in ((20, math.nan), (21, math.inf), (22, -math.inf)):
+            x[t, 4] = bad
+            e[t] = -1
+        x[23], e[23] = math.nan, 16
+        out = hc.balance_loss([x], [e], 4, **WEIGHTS)
+        (d,) = hc.balance_loss_backward([x], [e], out.coef)
+        assert torch.isfinite(out.loss).all() and torch.isfinite(d).all()
+        clean = x.clone()
+        clean[20:24] = 0
+        check([clean], [e], 4, out, [d])
+        assert (d[6] == 0).all()
+        x[30, 3] = math.nan                                  # a token that counts
+        out = hc.balance_loss([x], [e], 4, **WEIGHTS)
+        (d,) = hc.balance_loss_backward([x], [e], out.coef)
+        assert torch.isnan(out.loss).all() and torch.isnan(d[30]).all() and torch.isfinite(torch.cat([d[:30], d[31:]])).all()
+        x[30, 3] = math.inf
+        out = hc.balance_loss([x], [e], 4, **WEIGHTS)
+        assert torch.isnan(out.loss).all()
+
+
+def test_choices_that_are_no_expert():
+    x, e = batch(1, 8, 16, 3)
+    e[0] = torch.tensor([2, 2, 2])                            # the same expert three times: three choices, one token
+    e[1] = torch.tensor([-1, -(1 << 40), 1 << 40])            # padding
+    e[2] = torch.tensor([(1 << 32) + 3, 5, 16])               # low bits that look like one
+    out = hc.balance_loss([x], [e], 4, **WEIGHTS)
+    check([x], [e], 4, out, hc.balance_loss_backward([x], [e], out.coef))
+
+
+def test_counts_are_the_dispatch_of_an_all_to_all():
+    """rank_tokens of one batch a rank times the hidden size are the
+    workload's all-to-all(v) counts."""
+    import workloads as W
+    R, T, E, hidden = 8, 300, 64, 2048
+    routing = W.a2a_routing(R, T, E, 6)
+    _, counts, _, _ = W.a2a_plan(routing, R, E, hidden)
+    es = [torch.from_numpy(r).cuda() for r in routing]
+    xs = [torch.randn(T, E, device="cuda") for _ in range(R)]
+    out = hc.balance_loss(xs, es, R)
+    assert (out.rank_tokens.flatten() * hidden).tolist() == counts
+    assert int(out.expert_tokens.sum()) == R * T * 6
+
+
+def test_views_and_guards():
+    """Logits and choices at element offsets, and nothing written outside."""
+    for dt in (torch.float32, torch.bfloat16):
+        T, E, k = 77, 30, 4
+        x, e = batch(2, T, E, k, dt, torch.int32, 0.2)
+        xs = torch.cat([x.new_zeros(1), x.flatten()])[1:].view(T, E)
+        es = torch.cat([e.new_zeros(3), e.flatten()])[3:].view(T, k)
+        out = hc.balance_loss([xs], [es], 5, **WEIGHTS)
+        check([x], [e], 5, out)
+        o = hc._Balance(hc.FP32 if dt == torch.float32 else hc.BF16, 4, E, k, 1)
+        whole = torch.full((T * E + 40,), 9.0, dtype=dt, device="cuda")
+        vp = ctypes.c_void_p * 1
+        size = whole.element_size()
+        st = hc.lib().hoccl_balance_loss_backward(vp(xs.data_ptr()), vp(es.data_ptr()), (ctypes.c_size_t * 1)(T), 1,
+                                                  ctypes.byref(o), out.coef.data_ptr(), None,
+                                                  vp(whole.data_ptr() + 3 * size), None)
+        assert st == hc.OK
+        torch.cuda.synchronize()
+        assert (whole[:3] == 9).all() and (whole[3 + T * E:] == 9).all()
+        check([x], [e], 5, out, [whole[3:3 + T * E].view(T, E)])
+
+
+def test_budgets_and_streams_give_the_same_bits():
+    xs, es = zip(*[batch(70 + b, 3000 - 500 * b, 48, 6, padding=0.1) for b in range(3)])
+    xs, es = list(xs), list(es)
+    runs = []
+    for wg, own in ((0, False), (1, False), (4, True), (0, True)):
+        hc.set_config(workgroups_per_step=wg)
+        stream = torch.cuda.Stream() if own else None
+        torch.cuda.synchronize()
+        out = hc.balance_loss(xs, es, 6, stream=stream, **WEIGHTS)
+        d = hc.balance_loss_backward(xs, es, out.coef, stream=stream)
+        assert wg == 0 or hc.last_stats()["workgroups_per_step"] <= wg
+        torch.cuda.synchronize()
+        runs.append([*out, *d])
+    for other in runs[1:]:
+        for a, b in zip(runs[0], other):
+            assert torch.equal(a, b)
+
+
+def test_replays():
+    x, e = batch(80, 900, 64, 6, padding=0.1)
+    g = torch.ones(1, device="cuda")
+    hc.init()
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        out = hc.balance_loss([x], [e], 8, **WEIGHTS)
+        d = hc.balance_loss_backward([x], [e], out.coef, g)
+    for k in range(3):
+        y, f = batch(90 + k, 900, 64, 6, padding=0.1)
+        x.copy_(y)
+        e.copy_(f)
+        g.fill_(1.0 + k)
+        graph.replay()
+        torch.cuda.synchronize()
+        eager = hc.balance_loss([y], [f], 8, **WEIGHTS)
+        ed = hc.balance_loss_backward([y], [f], eager.coef, g)
+        torch.cuda.synchronize()
+        for a, b in zip([*out, *d], [*eager, *ed]):
+            assert torch.equal(a, b), k
+        check([y], [f], 8, out, d, g)
+    del graph
