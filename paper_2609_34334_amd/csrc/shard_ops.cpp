@@ -298,6 +298,10 @@ hoccl_status_t fill_balance(const hoccl_balance_t &o, const void *const *logits,
     a.nseg = batches;
     a.E = o.experts, a.k = o.topk, a.D = o.ranks;
     a.index64 = o.index_bytes == 8;
+    // 2^21 over the experts of a rank, rounded up: e times it is off by less
+    // than 2^10, which keeps e / experts-of-a-rank exact below 1024.
+    const uint32_t per = (uint32_t)(o.experts / o.ranks);
+    a.rank_mul = ((1u << 21) + per - 1) / per;
     a.expert_weight = o.expert_weight, a.rank_weight = o.rank_weight, a.traffic_weight = o.traffic_weight;
     a.max_ranks = o.max_ranks > 0 ? o.max_ranks : std::min(o.topk, o.ranks);
     return HOCCL_OK;
@@ -322,8 +326,7 @@ hoccl_status_t balance_loss(const void *const *logits, const void *const *choice
     TRY(mem.add(workspace, need, 4, true, "workspace"));
     TRY(mem.check());
     for (int b = 0; b < batches; ++b) a.first[b + 1] = a.first[b] + balance_blocks(tokens[b], o.experts, batches);
-    a.partial_p = (float *)workspace;
-    a.partial_n = (int32_t *)workspace + (size_t)a.first[batches] * (size_t)o.experts;
+    a.partial = (int32_t *)workspace;
     a.loss = loss, a.expert_tokens = expert_tokens, a.rank_tokens = rank_tokens, a.coef = coef;
 
     OpCall call;

@@ -100,8 +100,8 @@ struct BalanceArgs {
     uint32_t first[kMaxBatches + 1];  // first block of each batch
     int nseg, E, k, D;
     int index64;
-    float *partial_p;      // [blocks][E]
-    int32_t *partial_n;    // [blocks][E + D + 1]: choices, tokens a rank, tokens
+    uint32_t rank_mul;     // e * rank_mul >> 21 is the rank of expert e < 1024
+    int32_t *partial;      // [blocks][2 E + D + 1]: sums of p (floats), choices, tokens a rank, tokens
     float *loss;           // [nseg]
     int32_t *expert_tokens, *rank_tokens;  // [nseg][E], [nseg][D]
     float *coef;           // [nseg][E]

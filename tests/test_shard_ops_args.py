@@ -75,9 +75,9 @@ def test_adamw_python():
         hc.adamw(p, g * 2, m, v, step=1, lr=0.1)
     with pytest.raises(TypeError, match="fp32 or bf16"):
         hc.adamw([p[0].half()], g, m, v, step=1, lr=0.1)
-    with pytest.raises(TypeError, match=r"exp_avgs\[0\]"):
+    with pytest.raises(TypeError, match="exp_avgs"):
         hc.adamw(p, g, [m[0].half()], v, step=1, lr=0.1)
-    with pytest.raises(ValueError, match="shape"):
+    with pytest.raises(ValueError, match="elements"):
         hc.adamw(p, [torch.zeros(5)], m, v, step=1, lr=0.1)
     with pytest.raises(ValueError, match="contiguous"):
         hc.adamw(p, [torch.zeros(8)[::2]], m, v, step=1, lr=0.1)
