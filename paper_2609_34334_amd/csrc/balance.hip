@@ -29,6 +29,7 @@
 //
 // Bound by memory at many tokens (logits and choices read once, gradients
 // written), by the launches and the last sum's latency at few.
+#include <algorithm>
 #include <type_traits>
 
 #include "lanes.h"
@@ -40,6 +41,11 @@ namespace {
 constexpr int kThreads = 512;  // of the forward pass's first kernel
 constexpr int kWaves = kThreads / 64;
 constexpr int kAhead = 2;      // tokens of a lane in flight
+// Workgroups of the forward pass, and half of them at most for one batch:
+// two a CU, which is what its registers hold.  Every workgroup makes as many
+// passes as the others, whatever the batches' lengths (eight batches of 9,800
+// to 32,768 tokens, 256 experts: 51 us with as many workgroups for each).
+constexpr size_t kBlocks = 512;
 constexpr float kLog2e = 1.4426950408889634f;
 
 int lanes_of(int E) {
@@ -48,27 +54,35 @@ int lanes_of(int E) {
     return l;
 }
 
-__device__ __forceinline__ int choice(const BalanceArgs &a, const BalanceSeg &s, uint64_t i) {
-    // What does not fit in 31 bits is no expert either.
+// Choice i behind `experts`, -1 where it is no expert.
+__device__ __forceinline__ int choice(const BalanceArgs &a, const char *experts, uint32_t i) {
     if (a.index64) {
-        const int64_t v = ((const int64_t *)s.experts)[i];
-        return v >= 0 && v < a.E ? (int)v : -1;
+        const uint64_t v = ((const uint64_t *)experts)[i];
+        return v < (uint64_t)a.E ? (int)v : -1;
     }
-    const int32_t v = ((const int32_t *)s.experts)[i];
-    return v >= 0 && v < a.E ? v : -1;
+    const uint32_t v = ((const uint32_t *)experts)[i];
+    return v < (uint32_t)a.E ? (int)v : -1;
 }
 
 // A lane's logits of one token: NV vectors of VE, L lanes apart.
 template <class T, int L, int N>
 struct Logits {
     static constexpr int VE = 16 / T::size, NV = N / VE;
-    float v[NV][VE];
-    static __device__ __forceinline__ int at(int j, int lane) { return (j * L + lane) * VE; }
-    // `E`: 0 reads nothing.
-    __device__ __forceinline__ void load(const void *p, int lane, int E) {
+    // As they are read, and as numbers.
+    struct Packed {
+        Raw<16> v[NV];
+        // `E`: 0 reads nothing.
+        __device__ __forceinline__ void load(const void *p, int lane, int E) {
 #pragma unroll
-        for (int j = 0; j < NV; ++j) load_some<T>(p, at(j, lane), E, v[j]);
+            for (int j = 0; j < NV; ++j) load_vector<T>(p, at(j, lane), E, v[j]);
+        }
+    };
+    float v[NV][VE];
+    __device__ __forceinline__ explicit Logits(const Packed &x) {
+#pragma unroll
+        for (int j = 0; j < NV; ++j) T::template unpack<VE>(x.v[j], v[j]);
     }
+    static __device__ __forceinline__ int at(int j, int lane) { return (j * L + lane) * VE; }
     __device__ __forceinline__ void store(void *p, int lane, int E) const {
 #pragma unroll
         for (int j = 0; j < NV; ++j) store_some<T>(p, at(j, lane), E, v[j]);
@@ -120,7 +134,7 @@ __global__ void __launch_bounds__(kThreads) balance_kernel(BalanceArgs) {
     __shared__ int sum_n[L * N];
     __shared__ int sum_sent[64];
     __shared__ int sum_live;
-    const int E = a.E, D = a.D, k = a.k, stride = 2 * E + D + 1;
+    const int E = a.E, D = a.D, k = a.k, stride = balance_columns(E, D);
     const int lane = threadIdx.x % L, slot = threadIdx.x / L;
     for (uint32_t block = blockIdx.x; block < a.first[a.nseg]; block += gridDim.x) {
         uint32_t lb, nb;
@@ -131,27 +145,39 @@ __global__ void __launch_bounds__(kThreads) balance_kernel(BalanceArgs) {
         __syncthreads();
         float acc[X::NV][X::VE] = {};
         int sent[OWN] = {}, live = 0;
-        for (uint64_t row0 = (uint64_t)lb * ROWS * kAhead; row0 < s.tokens; row0 += (uint64_t)nb * ROWS * kAhead) {
-            // Every lane stays for the exchanges; a row behind the last
-            // reads nothing and is padding.
-            X x[kAhead];
-            int first[kAhead];  // the lane's first choice
+        // What a pass reads is loaded during the pass before it.
+        typename X::Packed next[kAhead];
+        int next_first[kAhead];  // the lane's first choice of each token
+        auto load = [&](uint64_t row0) {
+            const char *logits = (const char *)s.logits + row0 * E * T::size;
+            const char *experts = (const char *)s.experts + row0 * k * (a.index64 ? 8 : 4);
+            const uint64_t left = row0 < s.tokens ? s.tokens - row0 : 0;
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                const uint64_t row = row0 + u * ROWS + slot;
-                const bool in = row < s.tokens;
-                x[u].load((const char *)s.logits + row * E * T::size, lane, in ? E : 0);
-                first[u] = in && lane < k ? choice(a, s, row * k + lane) : -1;
+                // A row behind the last reads nothing and is padding.
+                const uint32_t row = u * ROWS + slot;
+                const bool in = row < left;
+                next[u].load(logits + row * (uint32_t)E * T::size, lane, in ? E : 0);
+                next_first[u] = in && lane < k ? choice(a, experts, row * k + lane) : -1;
             }
+        };
+        const uint64_t step = (uint64_t)nb * ROWS * kAhead;
+        uint64_t row0 = (uint64_t)lb * ROWS * kAhead;
+        if (row0 < s.tokens) load(row0);
+        for (; row0 < s.tokens; row0 += step) {
+            typename X::Packed now[kAhead];
+            int first[kAhead];
+#pragma unroll
+            for (int u = 0; u < kAhead; ++u) now[u] = next[u], first[u] = next_first[u];
+            if (row0 + step < s.tokens) load(row0 + step);
+            const char *experts = (const char *)s.experts + row0 * k * (a.index64 ? 8 : 4);
+            const uint64_t left = s.tokens - row0;
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                const uint64_t row = row0 + u * ROWS + slot;
-                const bool in = row < s.tokens;
+                const uint32_t row = u * ROWS + slot;
                 uint32_t lo = 0, hi = 0;  // the ranks that the token goes to
-                bool any = false;
                 auto choose = [&](int e) {
                     if (e < 0) return;
-                    any = true;
                     const uint32_t d = ((uint32_t)e * a.rank_mul) >> 21;
                     if (d < 32) lo |= 1u << d;
                     else hi |= 1u << (d - 32);
@@ -159,21 +185,22 @@ __global__ void __launch_bounds__(kThreads) balance_kernel(BalanceArgs) {
                 };
                 choose(first[u]);
                 for (int c = lane + L; c < k; c += L)
-                    if (in) choose(choice(a, s, row * k + c));
-                const bool valid = join_lanes<L, LaneOr>((uint32_t)any) != 0;
+                    if (row < left) choose(choice(a, experts, row * k + c));
                 lo = join_lanes<L, LaneOr>(lo);
                 if (D > 32) hi = join_lanes<L, LaneOr>(hi);
-                if (lane == 0) live += valid;
+                if ((lo | hi) == 0) continue;  // padding, for all of the token's lanes
+                if (lane == 0) ++live;
 #pragma unroll
                 for (int i = 0; i < OWN; ++i) {
                     const int d = i * L + lane;
                     sent[i] += ((d < 32 ? lo : hi) >> (d & 31)) & 1u;
                 }
-                const float inv = x[u].softmax(lane, E);
+                X x(now[u]);
+                const float inv = x.softmax(lane, E);
 #pragma unroll
                 for (int j = 0; j < X::NV; ++j)
 #pragma unroll
-                    for (int i = 0; i < X::VE; ++i) acc[j][i] += valid ? x[u].v[j][i] * inv : 0.0f;
+                    for (int i = 0; i < X::VE; ++i) acc[j][i] += x.v[j][i] * inv;
             }
         }
         // The wave's groups, then the waves in order.
@@ -210,45 +237,47 @@ __global__ void __launch_bounds__(kThreads) balance_kernel(BalanceArgs) {
 // Loss, weights and counts of a batch from its blocks' sums.  The sums of p,
 // the counts of choices, of tokens a rank and of tokens are columns of one
 // table with a row a block; all are added in 64 bits, where the counts are
-// exact.  Lots of rows are added side by side, eight rows of each in flight,
-// then the lots in order: one row after another, 64 blocks took 35 us, all
-// latency.
+// exact.  Lots of rows are added side by side, four columns a thread and eight
+// rows of them in flight, then the lots in order: one row and column after
+// another, 64 blocks took 35 us, all latency; a column a thread 11 (256
+// experts).
 constexpr int kFinishThreads = 1024;
-constexpr int kColumns = 2 * kMaxExperts + 64 + 1;
+constexpr int kColumns = 2 * kMaxExperts + 64 + 4;
 __global__ void __launch_bounds__(kFinishThreads) balance_finish_kernel(BalanceArgs) {
     const BalanceArgs &a = kernel_args<BalanceArgs>();
-    __shared__ double lot[kFinishThreads];
+    __shared__ double lot[kFinishThreads][4];
     __shared__ double tot[kColumns];
     __shared__ double rank_choices[64];
     __shared__ double red[kFinishThreads / 64][2];
-    const int E = a.E, D = a.D, per = E / D, cols = 2 * E + D + 1, t = threadIdx.x;
-    const int wide = (cols + 63) / 64 * 64;
-    const int lots = wide < kFinishThreads ? kFinishThreads / wide : 1;
+    const int E = a.E, D = a.D, per = E / D, cols = balance_columns(E, D), t = threadIdx.x;
+    const int wide = cols / 4, lots = kFinishThreads / wide, g = t / wide, c = t % wide * 4;
     for (int seg = blockIdx.x; seg < a.nseg; seg += gridDim.x) {
         const uint32_t nb = a.first[seg + 1] - a.first[seg];
-        const int32_t *rows = a.partial + (uint64_t)a.first[seg] * cols;
-        const int g = lots > 1 ? t / wide : 0;
-        for (int c = lots > 1 ? t % wide : t; c < cols; c += lots > 1 ? wide : kFinishThreads) {
-            if (g >= lots) break;
-            double sum = 0.0;
+        const int32_t *rows = a.partial + (uint64_t)a.first[seg] * cols + c;
+        if (g < lots) {
+            double sum[4] = {};
             for (uint32_t b0 = g; b0 < nb; b0 += 8 * lots) {
-                int32_t v[8];
+                Raw<16> v[8];
 #pragma unroll
                 for (int i = 0; i < 8; ++i) {
                     const uint32_t b = b0 + i * lots;
-                    v[i] = b < nb ? rows[(uint64_t)b * cols + c] : 0;
+                    if (b < nb) load_raw(v[i], rows + (uint64_t)b * cols);
+                    else v[i] = {};
                 }
 #pragma unroll
-                for (int i = 0; i < 8; ++i) sum += c < E ? (double)__int_as_float(v[i]) : (double)v[i];
+                for (int i = 0; i < 8; ++i)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        sum[j] += c + j < E ? (double)__uint_as_float(v[i].w[j]) : (double)(int32_t)v[i].w[j];
             }
-            if (lots > 1) lot[t] = sum;
-            else tot[c] = sum;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) lot[t][j] = sum[j];
         }
         __syncthreads();
-        if (lots > 1 && t < cols) {
-            double sum = lot[t];
-            for (int i = 1; i < lots; ++i) sum += lot[i * wide + t];
-            tot[t] = sum;
+        for (int i = t; i < cols; i += kFinishThreads) {
+            double sum = 0.0;
+            for (int l = 0; l < lots; ++l) sum += lot[l * wide + i / 4][i % 4];
+            tot[i] = sum;
         }
         __syncthreads();
         for (int e = t; e < E; e += kFinishThreads) a.expert_tokens[(uint64_t)seg * E + e] = (int32_t)tot[E + e];
@@ -303,37 +332,42 @@ __global__ void __launch_bounds__(kOpThreads) balance_backward_kernel(BalanceArg
         for (int j = 0; j < X::NV; ++j) load_some<EF32>(a.coef + (uint64_t)seg * E, X::at(j, lane), E, w[j]);
         const float g = a.grad ? a.grad[seg] : 1.0f;
         for (uint64_t row0 = (uint64_t)lb * ROWS * kAhead; row0 < s.tokens; row0 += (uint64_t)nb * ROWS * kAhead) {
-            X x[kAhead];
+            const char *logits = (const char *)s.logits + row0 * E * T::size;
+            const char *experts = (const char *)s.experts + row0 * k * (a.index64 ? 8 : 4);
+            char *dlogits = (char *)s.dlogits + row0 * E * T::size;
+            const uint64_t left = s.tokens - row0;
+            typename X::Packed now[kAhead];
             bool any[kAhead];
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                const uint64_t row = row0 + u * ROWS + slot;
-                const bool in = row < s.tokens;
-                x[u].load((const char *)s.logits + row * E * T::size, lane, in ? E : 0);
-                any[u] = in && lane < k && choice(a, s, row * k + lane) >= 0;
+                const uint32_t row = u * ROWS + slot;
+                const bool in = row < left;
+                now[u].load(logits + row * (uint32_t)E * T::size, lane, in ? E : 0);
+                any[u] = in && lane < k && choice(a, experts, row * k + lane) >= 0;
             }
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                const uint64_t row = row0 + u * ROWS + slot;
-                const bool in = row < s.tokens;
-                for (int c = lane + L; c < k; c += L) any[u] |= in && choice(a, s, row * k + c) >= 0;
+                const uint32_t row = u * ROWS + slot;
+                const bool in = row < left;
+                for (int c = lane + L; c < k; c += L) any[u] |= in && choice(a, experts, row * k + c) >= 0;
                 const bool valid = join_lanes<L, LaneOr>((uint32_t)any[u]) != 0;
-                const float inv = x[u].softmax(lane, E);
+                X x(now[u]);
+                const float inv = x.softmax(lane, E);
                 float dot = 0.0f;
 #pragma unroll
                 for (int j = 0; j < X::NV; ++j)
 #pragma unroll
                     for (int i = 0; i < X::VE; ++i) {
-                        x[u].v[j][i] *= inv;
-                        dot += x[u].v[j][i] * w[j][i];
+                        x.v[j][i] *= inv;
+                        dot += x.v[j][i] * w[j][i];
                     }
                 dot = join_lanes<L, LaneSum>(dot);
 #pragma unroll
                 for (int j = 0; j < X::NV; ++j)
 #pragma unroll
                     for (int i = 0; i < X::VE; ++i)
-                        x[u].v[j][i] = valid ? g * x[u].v[j][i] * (w[j][i] - dot) : 0.0f;
-                x[u].store((char *)s.dlogits + row * E * T::size, lane, in ? E : 0);
+                        x.v[j][i] = valid ? g * x.v[j][i] * (w[j][i] - dot) : 0.0f;
+                x.store(dlogits + row * (uint32_t)E * T::size, lane, in ? E : 0);
             }
         }
     }
@@ -357,16 +391,19 @@ const void *with_lanes(hoccl_dtype_t dt, int E, F &&f) {
 #undef HOCCL_LANES
 }
 
-// Workgroups of one batch, a pass each up to `most` of them.
-uint32_t blocks_of(size_t tokens, int E, int threads, size_t most) {
-    const size_t rows = (size_t)(threads / lanes_of(E) * kAhead), n = (tokens + rows - 1) / rows;
-    return (uint32_t)(n < 1 ? 1 : n < most ? n : most);
-}
+size_t rows_of(int E, int threads) { return (size_t)(threads / lanes_of(E) * kAhead); }
+size_t over(size_t n, size_t d) { return (n + d - 1) / d; }
 
 }  // namespace
 
-uint32_t balance_blocks(size_t tokens, int E, int batches) {
-    return blocks_of(tokens, E, kThreads, batches <= 2 ? 256 : batches < 32 ? 512 / batches : 16);
+void balance_blocks(const size_t *tokens, int E, int batches, uint32_t *first) {
+    const size_t rows = rows_of(E, kThreads);
+    size_t all = 0, longest = 0;
+    for (int b = 0; b < batches; ++b) all += over(tokens[b], rows), longest = std::max(longest, tokens[b]);
+    const size_t passes = std::max({(size_t)1, over(all, kBlocks), over(over(longest, rows), kBlocks / 2)});
+    first[0] = 0;
+    for (int b = 0; b < batches; ++b)
+        first[b + 1] = first[b] + (uint32_t)std::max((size_t)1, over(tokens[b], rows * passes));
 }
 
 hipError_t launch_balance(const BalanceArgs &a, hoccl_dtype_t dt, int wg, hipStream_t s) {
@@ -382,7 +419,9 @@ hipError_t launch_balance_finish(const BalanceArgs &a, int wg, hipStream_t s) {
     return hipLaunchKernel((const void *)balance_finish_kernel, dim3((unsigned)wg), dim3(kFinishThreads), args, 0, s);
 }
 
-uint32_t balance_backward_blocks(size_t tokens, int E) { return blocks_of(tokens, E, kOpThreads, 4096); }
+uint32_t balance_backward_blocks(size_t tokens, int E) {
+    return (uint32_t)std::min((size_t)4096, std::max((size_t)1, over(tokens, rows_of(E, kOpThreads))));
+}
 
 hipError_t launch_balance_backward(const BalanceArgs &a, hoccl_dtype_t dt, int wg, hipStream_t s) {
     const void *k = with_lanes(dt, a.E, [](auto t, auto l, auto n) {

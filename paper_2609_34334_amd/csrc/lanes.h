@@ -99,6 +99,25 @@ struct EBF16 {
     }
 };
 
+// A vector of 16 bytes of `p` from element e on; elements at and behind `end`
+// are zeros and are not read.
+template <class T, typename I>
+__device__ __forceinline__ void load_vector(const void *p, I e, I end, Raw<16> &r) {
+    constexpr int N = 16 / T::size;
+    if (e + N <= end) {
+        load_raw(r, (const char *)p + (size_t)e * T::size);
+    } else {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) r.w[i] = 0;
+#pragma unroll
+        for (int i = 0; i < N; ++i)
+            if (e + i < end) {
+                if constexpr (T::size == 4) r.w[i] = ((const uint32_t *)p)[e + i];
+                else r.w[i / 2] |= (uint32_t)((const uint16_t *)p)[e + i] << (16 * (i % 2));
+            }
+    }
+}
+
 // N elements of `p` from element e on; those at and behind `end` are zeros
 // and are not read.
 template <class T, bool NT = false, int N, typename I>
@@ -151,7 +170,8 @@ __device__ __forceinline__ float dpp(float v) {
 }
 
 // v of every lane joined over each aligned group of L lanes (a power of two
-// up to 64), the result in all of them.  Every lane has to take part.  Groups
+// up to 64), the result in all of them.  A group's lanes take part together;
+// other groups need not.  Groups
 // of up to 16 exchange by DPP: neighbours, pairs, then the mirrored half row
 // and the mirrored row (a group's lanes hold the same value by then, so that
 // a mirror is as good as an exchange); rows by the swaps of rows.

@@ -275,9 +275,9 @@ hoccl_status_t check_balance(const hoccl_balance_t *op, const size_t *tokens, in
 }
 
 size_t balance_workspace(const hoccl_balance_t &o, const size_t *tokens, int batches) {
-    size_t blocks = 0;
-    for (int b = 0; b < batches; ++b) blocks += balance_blocks(tokens[b], o.experts, batches);
-    return blocks * (size_t)(2 * o.experts + o.ranks + 1) * 4;
+    uint32_t first[kMaxBatches + 1];
+    balance_blocks(tokens, o.experts, batches, first);
+    return (size_t)first[batches] * (size_t)balance_columns(o.experts, o.ranks) * 4;
 }
 
 // The operands that both directions have.
@@ -325,7 +325,7 @@ hoccl_status_t balance_loss(const void *const *logits, const void *const *choice
     TRY(mem.add(coef, nb * (size_t)o.experts * 4, 4, true, "coef"));
     TRY(mem.add(workspace, need, 4, true, "workspace"));
     TRY(mem.check());
-    for (int b = 0; b < batches; ++b) a.first[b + 1] = a.first[b] + balance_blocks(tokens[b], o.experts, batches);
+    balance_blocks(tokens, o.experts, batches, a.first);
     a.partial = (int32_t *)workspace;
     a.loss = loss, a.expert_tokens = expert_tokens, a.rank_tokens = rank_tokens, a.coef = coef;
 

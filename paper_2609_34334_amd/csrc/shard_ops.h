@@ -101,7 +101,7 @@ struct BalanceArgs {
     int nseg, E, k, D;
     int index64;
     uint32_t rank_mul;     // e * rank_mul >> 21 is the rank of expert e < 1024
-    int32_t *partial;      // [blocks][2 E + D + 1]: sums of p (floats), choices, tokens a rank, tokens
+    int32_t *partial;      // [blocks][balance_columns]: sums of p (floats), choices, tokens a rank, tokens
     float *loss;           // [nseg]
     int32_t *expert_tokens, *rank_tokens;  // [nseg][E], [nseg][D]
     float *coef;           // [nseg][E]
@@ -110,7 +110,11 @@ struct BalanceArgs {
     int max_ranks;
 };
 
-uint32_t balance_blocks(size_t tokens, int E, int batches);
+// Words of a block's sums: E of p, E + D + 1 counts, and up to four's multiple.
+constexpr int balance_columns(int E, int D) { return (2 * E + D + 1 + 3) & ~3; }
+// Fills first[0 .. batches] with the blocks of the forward pass, a division
+// that goes by the sizes alone.
+void balance_blocks(const size_t *tokens, int E, int batches, uint32_t *first);
 hipError_t launch_balance(const BalanceArgs &a, hoccl_dtype_t dt, int wg, hipStream_t s);
 hipError_t launch_balance_finish(const BalanceArgs &a, int wg, hipStream_t s);
 uint32_t balance_backward_blocks(size_t tokens, int E);
