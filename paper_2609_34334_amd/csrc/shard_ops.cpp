@@ -206,7 +206,7 @@ hoccl_status_t rmsnorm(const void *x, const void *residual, const void *weight, 
 
     OpCall call;
     TRY(call.open(stream));
-    const RmsArgs a = {x, residual, weight, residual_out, y, scale, rows, (uint32_t)hidden, wdt == HOCCL_BF16, (float)eps};
+    const RmsArgs a = {x, residual, weight, residual_out, y, scale, rows, (uint32_t)hidden, wdt == HOCCL_BF16, (float)eps, 0};
     const int wg = call.budget(rmsnorm_workgroups(rows, hidden, dt, call.cus()));
     TRY(call.launch(wg, [&] { return launch_rmsnorm(a, dt, wg, stream); }));
     call.done((unsigned long long)bytes * (1 + (residual != nullptr) + (residual_out != nullptr)) +
@@ -238,7 +238,7 @@ hoccl_status_t rmsnorm_backward(const void *dy, const void *dres, const void *h,
     TRY(call.open(stream));
     if (rows > 0) {
         const RmsBackArgs a = {dy, dres, h, weight, dx, dweight ? (float *)workspace : nullptr, rows, (uint32_t)hidden,
-                               blocks, wdt == HOCCL_BF16, (float)eps};
+                               blocks, wdt == HOCCL_BF16, (float)eps, 0};
         const int wg = call.budget(blocks);
         TRY(call.launch(wg, [&] { return launch_rmsnorm_backward(a, dt, wg, stream); }));
     }

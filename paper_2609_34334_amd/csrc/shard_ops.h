@@ -61,6 +61,7 @@ struct RmsArgs {
     uint32_t hidden;
     int weight_bf16;
     float eps;
+    uint32_t threads;         // of a row; set at the launch
 };
 struct RmsBackArgs {
     const void *dy, *dres, *h, *weight;
@@ -70,15 +71,16 @@ struct RmsBackArgs {
     uint32_t hidden, blocks;
     int weight_bf16;
     float eps;
+    uint32_t threads;         // of a row; set at the launch
 };
 
 // Workgroups of the automatic launch.
 unsigned long long rmsnorm_workgroups(size_t rows, size_t hidden, hoccl_dtype_t dt, int cus);
-hipError_t launch_rmsnorm(const RmsArgs &a, hoccl_dtype_t dt, int wg, hipStream_t s);
+hipError_t launch_rmsnorm(RmsArgs a, hoccl_dtype_t dt, int wg, hipStream_t s);
 // Partial sums of the weight's gradient: a number that goes by the sizes
 // alone, so that the result does not depend on the workgroups.
 uint32_t rmsnorm_backward_blocks(size_t rows, size_t hidden, hoccl_dtype_t dt);
-hipError_t launch_rmsnorm_backward(const RmsBackArgs &a, hoccl_dtype_t dt, int wg, hipStream_t s);
+hipError_t launch_rmsnorm_backward(RmsBackArgs a, hoccl_dtype_t dt, int wg, hipStream_t s);
 uint32_t rmsnorm_grad_workgroups(size_t hidden);
 hipError_t launch_rmsnorm_weight_grad(const float *partial, uint32_t blocks, uint32_t hidden, float *dweight, int wg,
                                       hipStream_t s);
