@@ -595,8 +595,9 @@ typedef struct {
  * half a step, 1/16 of a value: with beta2 near 1 a v that is a block's
  * largest follows its gradients, the others follow in such steps.  bf16
  * parameters are rounded likewise (2^-9): small updates need fp32
- * parameters, whose bf16 `copy` is then what the all-gather sends.  Tensors
- * of no elements are skipped; 48 tensors share a launch. */
+ * parameters, whose bf16 `copy` is then what the all-gather sends.  eps is 0
+ * or at least 2^-126.  Tensors of no elements are skipped; 48 tensors share
+ * a launch. */
 hoccl_status_t hoccl_adamw(const hoccl_adamw_tensor_t *tensors, int count, const hoccl_adamw_t *options,
                            hipStream_t stream);
 

@@ -240,10 +240,10 @@ __device__ __forceinline__ void from_e4m3(const Raw<N> &r, float (&f)[N]) {
         f[4 * i] = a[0], f[4 * i + 1] = a[1], f[4 * i + 2] = b[0], f[4 * i + 3] = b[1];
     }
 }
-template <int N, typename I>
+template <bool NT = false, int N, typename I>
 __device__ __forceinline__ void load_bytes(const void *p, I e, I end, Raw<N> &r) {
     if (e + N <= end) {
-        load_raw(r, (const char *)p + e);
+        load_raw<NT>(r, (const char *)p + e);
     } else {
 #pragma unroll
         for (int i = 0; i < N / 4; ++i) r.w[i] = 0;
@@ -252,10 +252,10 @@ __device__ __forceinline__ void load_bytes(const void *p, I e, I end, Raw<N> &r)
             if (e + i < end) r.w[i / 4] |= (uint32_t)((const uint8_t *)p)[e + i] << (8 * (i % 4));
     }
 }
-template <int N, typename I>
+template <bool NT = false, int N, typename I>
 __device__ __forceinline__ void store_bytes(void *p, I e, I end, const Raw<N> &r) {
     if (e + N <= end) {
-        store_raw((char *)p + e, r);
+        store_raw<NT>((char *)p + e, r);
     } else {
 #pragma unroll
         for (int i = 0; i < N; ++i)

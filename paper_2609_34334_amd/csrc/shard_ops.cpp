@@ -3,6 +3,7 @@
 #include "shard_ops.h"
 
 #include <algorithm>
+#include <cfloat>
 #include <cmath>
 #include <cstring>
 #include <vector>
@@ -100,6 +101,7 @@ hoccl_status_t check_adamw(const hoccl_adamw_t &o) {
         return invalid("betas %g, %g outside [0, 1)", o.beta1, o.beta2);
     if (!(o.eps >= 0 && std::isfinite(o.eps)) || !(o.weight_decay >= 0 && std::isfinite(o.weight_decay)))
         return invalid("eps %g or weight_decay %g negative or not finite", o.eps, o.weight_decay);
+    if (o.eps > 0 && o.eps < FLT_MIN) return invalid("eps = %g is neither 0 nor a normal fp32 number", o.eps);
     if ((uintptr_t)o.lr_dev % 4 || (uintptr_t)o.step_dev % 4 || (uintptr_t)o.grad_scale % 4)
         return invalid("lr_dev, step_dev and grad_scale are 4-byte elements");
     return HOCCL_OK;

@@ -34,7 +34,7 @@ ROW = (P, 2 * P, 3 * P, 4 * P, 0, 0, 0, 64)
 @pytest.mark.parametrize("kw", [
     dict(param_dtype=hc.INT32), dict(grad_dtype=hc.UINT8), dict(param_dtype=9), dict(state_bits=16), dict(step=0),
     dict(step=-3), dict(lr=-1.0), dict(lr=float("nan")), dict(lr=float("inf")), dict(beta1=1.0), dict(beta1=-0.1),
-    dict(beta2=1.0), dict(beta2=float("nan")), dict(eps=-1e-8), dict(eps=float("nan")), dict(weight_decay=-1.0),
+    dict(beta2=1.0), dict(beta2=float("nan")), dict(eps=-1e-8), dict(eps=float("nan")), dict(eps=1e-40), dict(weight_decay=-1.0),
     dict(weight_decay=float("inf")), dict(lr_dev=P + 2), dict(step_dev=P + 1), dict(grad_scale=P + 3)])
 def test_adamw_options(kw):
     assert adamw([ROW], **kw) == BAD
