@@ -1,7 +1,8 @@
 """Python binding of libhoccl (ctypes).
 
 Argument marshalling only: every step of a collective runs in the HIP
-library (``libhoccl.so``, built from ``csrc/`` by ``build.py``).  PyTorch is
+library (``libhoccl.so``, built from ``csrc/`` by ``build.py``; so is
+``_tensors.so``, which reads lists of tensors).  PyTorch is
 used for device memory and streams; each call passes raw device pointers and
 ``torch.cuda.current_stream().cuda_stream`` (or the stream given) to the
 C ABI declared in ``include/hoccl.h``.
@@ -13,7 +14,6 @@ import array
 import collections
 import contextlib
 import ctypes
-import operator
 import os
 import threading
 
@@ -22,10 +22,13 @@ import torch
 _HERE = os.path.dirname(os.path.abspath(__file__))
 LIB_PATH = os.path.join(_HERE, "libhoccl.so")
 
-if not os.path.exists(LIB_PATH):
-    raise ImportError(
-        f"{LIB_PATH} is not built; run `python -m paper_2609_34334_amd.build` "
-        "(or __graft_entry__.build()) first")
+for _path in (LIB_PATH, os.path.join(_HERE, "_tensors.so")):
+    if not os.path.exists(_path):
+        raise ImportError(
+            f"{_path} is not built; run `python -m paper_2609_34334_amd.build` "
+            "(or __graft_entry__.build()) first")
+
+from . import _tensors  # noqa: E402  (csrc/tensors.cpp)
 
 _lib = ctypes.CDLL(LIB_PATH)
 
@@ -561,45 +564,48 @@ _FLOATS = {torch.float32: FP32, torch.bfloat16: BF16}
 _NOWHERE = contextlib.nullcontext()
 
 
-def _at(device, stream):
-    """The context of a call on `device`: that GPU current and, given a
-    stream, the stream too, so that what the call allocates belongs to it."""
-    if device.type != "cuda":
-        raise ValueError("tensors must live on a GPU")
-    if stream is None:
-        return _NOWHERE if torch.cuda.current_device() == device.index else torch.cuda.device(device)
-    if stream.device != device:
-        raise ValueError(f"the stream is on {stream.device}, the tensors on {device}")
-    return torch.cuda.stream(stream)
-
-
-# The current stream's handle without the Stream object around it, which takes
-# 2.6 us of a call's 12 to make.
+# The current device and the current stream's handle without the objects and
+# checks around them: 3.2 us of a call's 12.
+_current_device = getattr(torch._C, "_cuda_getDevice", torch.cuda.current_device)
 _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream",
                       lambda index: torch.cuda.current_stream(index).cuda_stream)
 
 
-def _handle(device, stream):
-    return _raw_stream(device.index) if stream is None else stream.cuda_stream
+def _at(index, stream):
+    """The context of a call on GPU `index` (a tensor's get_device()): that
+    GPU current and, given a stream, the stream too, so that what the call
+    allocates belongs to it."""
+    if index < 0:
+        raise ValueError("tensors must live on a GPU")
+    if stream is None:
+        return _NOWHERE if _current_device() == index else torch.cuda.device(index)
+    if stream.device.index != index:
+        raise ValueError(f"the stream is on {stream.device}, the tensors on GPU {index}")
+    return torch.cuda.stream(stream)
 
 
-def _want(t, name, device, dtypes, shape=None):
+def _handle(index, stream):
+    return _raw_stream(index) if stream is None else stream.cuda_stream
+
+
+def _want(t, name, index, dtypes, shape=None):
     """Checks one operand; returns its dtype's code (or None)."""
-    if t.dtype not in dtypes:
-        raise TypeError(f"{name} must be {' or '.join(map(str, dtypes))}, not {t.dtype}")
-    if t.device != device:
+    dtype = t.dtype
+    if dtype not in dtypes:
+        raise TypeError(f"{name} must be {' or '.join(map(str, dtypes))}, not {dtype}")
+    if t.get_device() != index:
         raise ValueError("all buffers must live on the same GPU")
     if not t.is_contiguous():
         raise ValueError("buffers must be contiguous")
     if shape is not None and t.shape != shape:
         raise ValueError(f"{name} has the shape {tuple(t.shape)}, not {tuple(shape)}")
-    return _FLOATS.get(t.dtype)
+    return _FLOATS.get(dtype)
 
 
-def _scalar(t, name, device, dtype):
+def _scalar(t, name, index, dtype):
     if t.numel() != 1:
         raise ValueError(f"{name} must have one element")
-    _want(t, name, device, (dtype,))
+    _want(t, name, index, (dtype,))
     return t.data_ptr()
 
 
@@ -620,31 +626,6 @@ def adamw_state(params, bits=32):
     return q(), q(), s(), s()
 
 
-def _address(a):
-    return a.buffer_info()[0]
-
-
-_dtypes = operator.attrgetter("dtype")
-_T = torch.Tensor
-
-
-def _column(ts, name, device, dtype, numels):
-    """Checks one list of operands; returns their addresses.  The lists may
-    hold hundreds of tensors, so each property is taken by one map over all of
-    them: 150 tensors of 6 lists take 0.2 ms, checked one by one 0.5."""
-    if len(ts) != len(numels):
-        raise ValueError(f"{name} has {len(ts)} tensors, params {len(numels)}")
-    if set(map(_dtypes, ts)) != {dtype}:
-        raise TypeError(f"{name} must all be {dtype}")
-    if set(map(_T.get_device, ts)) != {device}:
-        raise ValueError("all buffers must live on the same GPU")
-    if not all(map(_T.is_contiguous, ts)):
-        raise ValueError("buffers must be contiguous")
-    if list(map(_T.numel, ts)) != numels:
-        raise ValueError(f"{name} must have the params' numbers of elements (scales: one for each {BLOCK})")
-    return array.array("Q", map(_T.data_ptr, ts))
-
-
 def adamw(params, grads, exp_avgs, exp_avg_sqs, exp_avg_scales=None, exp_avg_sq_scales=None, *, step, lr,
           betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, copies=None, grad_scale=None, stream=None):
     """One AdamW step over lists of tensors, in place (hoccl_adamw).  All
@@ -662,37 +643,41 @@ def adamw(params, grads, exp_avgs, exp_avg_sqs, exp_avg_scales=None, exp_avg_sq_
         if len(grads) != n:
             raise ValueError(f"grads has {len(grads)} tensors, params {n}")
         return params
-    device, index = params[0].device, params[0].get_device()
-    pdt, gdt = params[0].dtype, grads[0].dtype
+    index, pdt, gdt = params[0].get_device(), params[0].dtype, grads[0].dtype
     if pdt not in _FLOATS or gdt not in _FLOATS:
         raise TypeError(f"params and grads must be fp32 or bf16, not {pdt} and {gdt}")
     states = torch.float8_e4m3fn if eight else torch.float32
-    numels = list(map(_T.numel, params))
+    numels = _tensors.numels(params)
+    counts = array.array("Q", numels)
     rows = array.array("Q", bytes(64 * n))       # hoccl_adamw_tensor_t: eight words
-    rows[0::8] = _column(params, "params", index, pdt, numels)
-    rows[1::8] = _column(grads, "grads", index, gdt, numels)
-    rows[2::8] = _column(exp_avgs, "exp_avgs", index, states, numels)
-    rows[3::8] = _column(exp_avg_sqs, "exp_avg_sqs", index, states, numels)
+
+    def column(word, name, ts, dtype, numels):
+        rows[word::8] = array.array("Q", _tensors.read(name, ts, dtype, index, numels))
+
+    column(0, "params", params, pdt, numels)
+    column(1, "grads", grads, gdt, numels)
+    column(2, "exp_avgs", exp_avgs, states, numels)
+    column(3, "exp_avg_sqs", exp_avg_sqs, states, numels)
     if eight:
-        blocks = [(k + BLOCK - 1) // BLOCK for k in numels]
-        rows[4::8] = _column(exp_avg_scales, "exp_avg_scales", index, torch.float32, blocks)
-        rows[5::8] = _column(exp_avg_sq_scales, "exp_avg_sq_scales", index, torch.float32, blocks)
+        blocks = array.array("Q", [(k + BLOCK - 1) // BLOCK for k in counts]).tobytes()
+        column(4, "exp_avg_scales", exp_avg_scales, torch.float32, blocks)
+        column(5, "exp_avg_sq_scales", exp_avg_sq_scales, torch.float32, blocks)
     if copies is not None:
-        rows[6::8] = _column(copies, "copies", index, torch.bfloat16, numels)
-    rows[7::8] = array.array("Q", numels)
-    with _at(device, stream):
+        column(6, "copies", copies, torch.bfloat16, numels)
+    rows[7::8] = counts
+    with _at(index, stream):
         o = _AdamW(_FLOATS[pdt], _FLOATS[gdt], 8 if eight else 32, 0, 0.0, betas[0], betas[1], eps, weight_decay)
-        if isinstance(step, _T):
-            o.step_dev = _scalar(step, "step", device, torch.int32)
+        if isinstance(step, torch.Tensor):
+            o.step_dev = _scalar(step, "step", index, torch.int32)
         else:
             o.step = step
-        if isinstance(lr, _T):
-            o.lr_dev = _scalar(lr, "lr", device, torch.float32)
+        if isinstance(lr, torch.Tensor):
+            o.lr_dev = _scalar(lr, "lr", index, torch.float32)
         else:
             o.lr = lr
         if grad_scale is not None:
-            o.grad_scale = _scalar(grad_scale, "grad_scale", device, torch.float32)
-        _check(_lib.hoccl_adamw(_address(rows), n, ctypes.byref(o), _handle(device, stream)), "hoccl_adamw")
+            o.grad_scale = _scalar(grad_scale, "grad_scale", index, torch.float32)
+        _check(_lib.hoccl_adamw(rows.buffer_info()[0], n, ctypes.byref(o), _handle(index, stream)), "hoccl_adamw")
     return params
 
 
@@ -710,37 +695,37 @@ def rmsnorm(x, weight, residual=None, *, eps=1e-6, quantize=False, out=None, res
     float8_e4m3fn values, shaped like x, and fp32 scales [..., blocks of
     BLOCK].  `out` (y, or the pair) and `residual_out` default to new tensors;
     y and residual_out may each be x or residual itself."""
-    device = x.device
-    dt = _want(x, "x", device, _FLOATS)
+    index = x.get_device()
+    dt = _want(x, "x", index, _FLOATS)
     rows, hidden = _rows(x)
-    wdt = _want(weight, "weight", device, _FLOATS, (hidden,))
+    wdt = _want(weight, "weight", index, _FLOATS, (hidden,))
     if residual is not None:
-        _want(residual, "residual", device, (x.dtype,), x.shape)
-    with _at(device, stream):
+        _want(residual, "residual", index, (x.dtype,), x.shape)
+    with _at(index, stream):
         q = scale = y = None
         if quantize:
             blocks = x.shape[:-1] + (-(-hidden // BLOCK),)
             if out is None:
-                q = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=device)
-                scale = torch.empty(blocks, dtype=torch.float32, device=device)
+                q = torch.empty(x.shape, dtype=torch.float8_e4m3fn, device=x.device)
+                scale = torch.empty(blocks, dtype=torch.float32, device=x.device)
             else:
                 q, scale = out
-                _want(q, "out", device, (torch.float8_e4m3fn,), x.shape)
-                _want(scale, "the scales of out", device, (torch.float32,), blocks)
+                _want(q, "out", index, (torch.float8_e4m3fn,), x.shape)
+                _want(scale, "the scales of out", index, (torch.float32,), blocks)
         else:
             y = torch.empty_like(x) if out is None else out
             if out is not None:
-                _want(y, "out", device, (x.dtype,), x.shape)
+                _want(y, "out", index, (x.dtype,), x.shape)
         if residual_out is None:
             if residual is not None:
                 residual_out = torch.empty_like(x)
         else:
-            _want(residual_out, "residual_out", device, (x.dtype,), x.shape)
+            _want(residual_out, "residual_out", index, (x.dtype,), x.shape)
         if rows:
             _check(_lib.hoccl_rmsnorm(x.data_ptr(), None if residual is None else residual.data_ptr(), weight.data_ptr(),
                                       None if residual_out is None else residual_out.data_ptr(),
                                       (q if quantize else y).data_ptr(), scale.data_ptr() if quantize else None,
-                                      rows, hidden, eps, dt, wdt, _handle(device, stream)), "hoccl_rmsnorm")
+                                      rows, hidden, eps, dt, wdt, _handle(index, stream)), "hoccl_rmsnorm")
     y = (q, scale) if quantize else y
     return y if residual is None else (y, residual_out)
 
@@ -751,32 +736,32 @@ def rmsnorm_backward(grad, h, weight, grad_residual=None, *, eps=1e-6, weight_gr
     (hoccl_rmsnorm_backward).  dx is the gradient of x and of the residual, in
     `out` (a new tensor; or grad, grad_residual or h itself); dweight is fp32,
     or None without `weight_grad`."""
-    device = h.device
-    dt = _want(h, "h", device, _FLOATS)
+    index = h.get_device()
+    dt = _want(h, "h", index, _FLOATS)
     rows, hidden = _rows(h)
-    wdt = _want(weight, "weight", device, _FLOATS, (hidden,))
-    _want(grad, "grad", device, (h.dtype,), h.shape)
+    wdt = _want(weight, "weight", index, _FLOATS, (hidden,))
+    _want(grad, "grad", index, (h.dtype,), h.shape)
     if grad_residual is not None:
-        _want(grad_residual, "grad_residual", device, (h.dtype,), h.shape)
+        _want(grad_residual, "grad_residual", index, (h.dtype,), h.shape)
     if out is not None:
-        _want(out, "out", device, (h.dtype,), h.shape)
-    with _at(device, stream):
+        _want(out, "out", index, (h.dtype,), h.shape)
+    with _at(index, stream):
         dx = torch.empty_like(h) if out is None else out
         dweight = ws = None
         need = ctypes.c_size_t(0)
         if weight_grad:
-            dweight = torch.empty(hidden, dtype=torch.float32, device=device)
+            dweight = torch.empty(hidden, dtype=torch.float32, device=h.device)
             if hidden:
                 _check(_lib.hoccl_rmsnorm_backward_workspace(rows, hidden, dt, ctypes.byref(need)),
                        "hoccl_rmsnorm_backward_workspace")
-            ws = torch.empty(need.value, dtype=torch.uint8, device=device)
+            ws = torch.empty(need.value, dtype=torch.uint8, device=h.device)
         if hidden:
             _check(_lib.hoccl_rmsnorm_backward(grad.data_ptr(),
                                                None if grad_residual is None else grad_residual.data_ptr(),
                                                h.data_ptr(), weight.data_ptr(), dx.data_ptr(),
                                                dweight.data_ptr() if weight_grad else None,
                                                ws.data_ptr() if weight_grad else None, need.value, rows, hidden, eps,
-                                               dt, wdt, _handle(device, stream)), "hoccl_rmsnorm_backward")
+                                               dt, wdt, _handle(index, stream)), "hoccl_rmsnorm_backward")
     return dx, dweight
 
 
@@ -787,24 +772,20 @@ def _balance(logits, experts, ranks, weights=(0.0, 0.0, 0.0), max_ranks=0):
     """The options and host arrays of both directions."""
     if not logits or len(logits) != len(experts):
         raise ValueError("logits and experts must be lists of the same length, one tensor a batch")
-    device, dtype, index = logits[0].device, logits[0].dtype, experts[0].dtype
+    dtype, choices = logits[0].dtype, experts[0].dtype
     if dtype not in _FLOATS:
         raise TypeError(f"logits must be fp32 or bf16, not {dtype}")
-    if index not in (torch.int32, torch.int64):
-        raise TypeError(f"experts must be int32 or int64, not {index}")
+    if choices not in (torch.int32, torch.int64):
+        raise TypeError(f"experts must be int32 or int64, not {choices}")
     if logits[0].dim() != 2 or experts[0].dim() != 2:
         raise ValueError("logits are [tokens, experts], experts [tokens, topk]")
     E, k = logits[0].shape[1], experts[0].shape[1]
-    n = len(logits)
-    lengths = [len(x) for x in logits]
-    if [x.shape for x in logits] != [(t, E) for t in lengths] or [e.shape for e in experts] != [(t, k) for t in lengths]:
-        raise ValueError("logits must have the shapes [tokens, experts], experts [tokens, topk] of the same tokens")
-    on = logits[0].get_device()
-    lp = _column(logits, "logits", on, dtype, [t * E for t in lengths])
-    ep = _column(experts, "experts", on, index, [t * k for t in lengths])
-    tokens = array.array("Q", lengths)
-    o = _Balance(_FLOATS[dtype], index.itemsize, E, k, ranks, max_ranks, *weights)
-    return device, o, tokens, lp, ep
+    tokens = _tensors.rows("logits", logits, E)
+    if _tensors.rows("experts", experts, k) != tokens:
+        raise ValueError("logits and experts must have the same tokens")
+    index = logits[0].get_device()
+    lp, ep = _tensors.read("logits", logits, dtype, index), _tensors.read("experts", experts, choices, index)
+    return index, _Balance(_FLOATS[dtype], choices.itemsize, E, k, ranks, max_ranks, *weights), tokens, lp, ep
 
 
 def balance_loss(logits, experts, ranks=1, *, expert_weight=1.0, rank_weight=0.0, traffic_weight=0.0, max_ranks=None,
@@ -816,19 +797,19 @@ def balance_loss(logits, experts, ranks=1, *, expert_weight=1.0, rank_weight=0.0
     Returns a BalanceLoss: loss [batches], expert_tokens [batches, E] and
     rank_tokens [batches, ranks] (int32: choices of an expert, tokens sent to
     a rank), and coef, which balance_loss_backward takes."""
-    device, o, tokens, lp, ep = _balance(logits, experts, ranks, (expert_weight, rank_weight, traffic_weight),
-                                         0 if max_ranks is None else max_ranks)
-    n = len(logits)
-    with _at(device, stream):
-        need = ctypes.c_size_t(0)
-        _check(_lib.hoccl_balance_workspace(_address(tokens), n, ctypes.byref(o), ctypes.byref(need)), "hoccl_balance_workspace")
+    index, o, tokens, lp, ep = _balance(logits, experts, ranks, (expert_weight, rank_weight, traffic_weight),
+                                        0 if max_ranks is None else max_ranks)
+    n, E = len(logits), o.experts
+    with _at(index, stream):
+        need, device, o_ = ctypes.c_size_t(0), logits[0].device, ctypes.byref(o)
+        _check(_lib.hoccl_balance_workspace(tokens, n, o_, ctypes.byref(need)), "hoccl_balance_workspace")
         ws = torch.empty(need.value, dtype=torch.uint8, device=device)
         loss = torch.empty(n, dtype=torch.float32, device=device)
-        counts = torch.empty(n, o.experts, dtype=torch.int32, device=device)
+        counts = torch.empty(n, E, dtype=torch.int32, device=device)
         sent = torch.empty(n, ranks, dtype=torch.int32, device=device)
-        coef = torch.empty(n, o.experts, dtype=torch.float32, device=device)
-        _check(_lib.hoccl_balance_loss(_address(lp), _address(ep), _address(tokens), n, ctypes.byref(o), loss.data_ptr(), counts.data_ptr(),
-                                       sent.data_ptr(), coef.data_ptr(), ws.data_ptr(), need.value, _handle(device, stream)),
+        coef = torch.empty(n, E, dtype=torch.float32, device=device)
+        _check(_lib.hoccl_balance_loss(lp, ep, tokens, n, o_, loss.data_ptr(), counts.data_ptr(), sent.data_ptr(),
+                                       coef.data_ptr(), ws.data_ptr(), need.value, _handle(index, stream)),
                "hoccl_balance_loss")
     return BalanceLoss(loss, counts, sent, coef)
 
@@ -836,15 +817,15 @@ def balance_loss(logits, experts, ranks=1, *, expert_weight=1.0, rank_weight=0.0
 def balance_loss_backward(logits, experts, coef, grad=None, *, stream=None):
     """The gradients of the logits, from balance_loss's coef and the gradient
     of its losses (fp32 [batches]; ones by default)."""
-    device, o, tokens, lp, ep = _balance(logits, experts, 1)
+    index, o, tokens, lp, ep = _balance(logits, experts, 1)
     n = len(logits)
-    _want(coef, "coef", device, (torch.float32,), (n, o.experts))
+    _want(coef, "coef", index, (torch.float32,), (n, o.experts))
     if grad is not None:
-        _want(grad, "grad", device, (torch.float32,), (n,))
-    with _at(device, stream):
+        _want(grad, "grad", index, (torch.float32,), (n,))
+    with _at(index, stream):
         out = [torch.empty_like(x) for x in logits]
-        dp = array.array("Q", map(_T.data_ptr, out))
-        _check(_lib.hoccl_balance_loss_backward(_address(lp), _address(ep), _address(tokens), n, ctypes.byref(o),
-                                                coef.data_ptr(), None if grad is None else grad.data_ptr(),
-                                                _address(dp), _handle(device, stream)), "hoccl_balance_loss_backward")
+        _check(_lib.hoccl_balance_loss_backward(lp, ep, tokens, n, ctypes.byref(o), coef.data_ptr(),
+                                                None if grad is None else grad.data_ptr(),
+                                                _tensors.read("out", out, out[0].dtype, index),
+                                                _handle(index, stream)), "hoccl_balance_loss_backward")
     return out

@@ -1,4 +1,5 @@
-"""Builds libhoccl.so in-tree with hipcc for gfx950.
+"""Builds libhoccl.so in-tree with hipcc for gfx950, and the extension module
+_tensors.so, which reads lists of torch tensors, with the host compiler.
 
 Every source is compiled to an object in parallel, then linked into
 ``paper_2609_34334_amd/libhoccl.so`` next to this file.  Always rebuilds.
@@ -6,12 +7,14 @@ Every source is compiled to an object in parallel, then linked into
 import os
 import subprocess
 import sys
+import sysconfig
 from concurrent.futures import ThreadPoolExecutor
 
 HERE = os.path.dirname(os.path.abspath(__file__))
 CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libhoccl.so")
+TENSORS = os.path.join(HERE, "_tensors.so")
 SOURCES = ["api.cpp", "plan.cpp", "proxy.cpp", "schedule.cpp", "kernels.hip", "handshake.hip",
            "scratch.hip", "ceilings.hip", "ipc.cpp", "mailbox.cpp", "shard_ops.cpp", "adamw.hip",
            "rmsnorm.hip", "balance.hip"]
@@ -33,10 +36,28 @@ def _compile(src):
     return obj
 
 
+def _tensors():
+    import torch
+    home = os.path.dirname(torch.__file__)
+    tmp = TENSORS + ".tmp"
+    cmd = [os.environ.get("CXX", "g++"), "-O2", "-std=c++17", "-fPIC", "-shared", "-Wall",
+           f"-D_GLIBCXX_USE_CXX11_ABI={int(torch._C._GLIBCXX_USE_CXX11_ABI)}",
+           "-isystem", os.path.join(home, "include"),
+           "-isystem", os.path.join(home, "include", "torch", "csrc", "api", "include"),
+           "-I" + sysconfig.get_paths()["include"], os.path.join(CSRC, "tensors.cpp"), "-o", tmp,
+           "-L" + os.path.join(home, "lib"), "-ltorch_python", "-ltorch_cpu", "-lc10"]
+    r = subprocess.run(cmd, capture_output=True, text=True)
+    if r.returncode != 0:
+        raise RuntimeError(f"building _tensors.so failed:\n{r.stdout}{r.stderr}")
+    os.replace(tmp, TENSORS)
+
+
 def build(verbose=True):
     os.makedirs(BUILD, exist_ok=True)
-    with ThreadPoolExecutor(max_workers=len(SOURCES)) as ex:
+    with ThreadPoolExecutor(max_workers=len(SOURCES) + 1) as ex:
+        tensors = ex.submit(_tensors)
         objs = list(ex.map(_compile, SOURCES))
+        tensors.result()
     tmp = LIB + ".tmp"
     cmd = [HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", tmp] + objs + [
         "-L/opt/rocm/lib", "-lhsa-runtime64", "-lamdhip64", "-pthread"]

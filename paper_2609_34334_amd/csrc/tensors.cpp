@@ -1,0 +1,144 @@
+// _tensors: reads lists of torch tensors for the Python binding.  An AdamW
+// step over 150 tensors of six lists asks 900 tensors for five properties
+// each; asked from Python that took 0.23 ms, here 0.01.
+//
+// read(name, tensors, dtype, device, numels=None): the tensors' addresses as
+// bytes (native 64-bit words), once all are contiguous tensors of `dtype` on
+// the GPU number `device` (-1: not on a GPU) and, where `numels` is given (as
+// numels() returns it), have those numbers of elements.  TypeError or
+// ValueError, naming the list, otherwise.
+// numels(tensors): their numbers of elements as bytes.
+// rows(name, tensors, columns): their first sizes as bytes, once all have two
+// dimensions, the second of `columns`; ValueError otherwise.
+#define PY_SSIZE_T_CLEAN
+#include <torch/csrc/Dtype.h>
+#include <torch/csrc/autograd/python_variable.h>
+
+#include <cstdint>
+#include <cstring>
+
+namespace {
+
+// f(i, tensor) of every tensor of a list or tuple; false where f is, or with
+// an error set.
+template <typename F>
+bool each(PyObject *seq, F &&f) {
+    const Py_ssize_t n = PySequence_Fast_GET_SIZE(seq);
+    for (Py_ssize_t i = 0; i < n; ++i) {
+        PyObject *o = PySequence_Fast_GET_ITEM(seq, i);
+        if (!THPVariable_Check(o)) {
+            PyErr_SetString(PyExc_TypeError, "a list of tensors is needed");
+            return false;
+        }
+        if (!f(i, THPVariable_Unpack(o))) return false;
+    }
+    return true;
+}
+
+// Runs f; a C++ exception becomes a Python one.
+template <typename F>
+PyObject *guarded(F &&f) {
+    try {
+        return f();
+    } catch (const std::exception &e) {
+        PyErr_SetString(PyExc_RuntimeError, e.what());
+    } catch (...) {
+        PyErr_SetString(PyExc_RuntimeError, "unexpected C++ exception");
+    }
+    return nullptr;
+}
+
+// Bytes of a 64-bit word a tensor, which f(i, tensor, word) fills; f returns
+// false with an error set.
+template <typename F>
+PyObject *words(PyObject *list, F &&f) {
+    PyObject *seq = PySequence_Fast(list, "a list of tensors is needed");
+    if (!seq) return nullptr;
+    PyObject *out = PyBytes_FromStringAndSize(nullptr, 8 * PySequence_Fast_GET_SIZE(seq));
+    PyObject *done = !out ? nullptr : guarded([&]() -> PyObject * {
+        const bool fine = each(seq, [&](Py_ssize_t i, const at::Tensor &t) {
+            int64_t word;
+            if (!f(i, t, word)) return false;
+            std::memcpy(PyBytes_AS_STRING(out) + 8 * i, &word, 8);
+            return true;
+        });
+        return fine ? out : nullptr;
+    });
+    Py_DECREF(seq);
+    if (!done) Py_XDECREF(out);
+    return done;
+}
+
+PyObject *read(PyObject *, PyObject *args) {
+    const char *name;
+    PyObject *list, *dtype, *numels = Py_None;
+    int device;
+    if (!PyArg_ParseTuple(args, "sOOi|O", &name, &list, &dtype, &device, &numels)) return nullptr;
+    const bool counted = numels != Py_None;
+    if (!THPDtype_Check(dtype) || (counted && !PyBytes_Check(numels))) {
+        PyErr_SetString(PyExc_TypeError, "read(name, tensors, dtype, device, numels=None)");
+        return nullptr;
+    }
+    const Py_ssize_t n = PySequence_Size(list);
+    if (n < 0) return nullptr;
+    if (counted && PyBytes_GET_SIZE(numels) != 8 * n) {
+        PyErr_Format(PyExc_ValueError, "%s has %zd tensors, not %zd", name, n, PyBytes_GET_SIZE(numels) / 8);
+        return nullptr;
+    }
+    const auto type = reinterpret_cast<THPDtype *>(dtype)->scalar_type;
+    return words(list, [&](Py_ssize_t i, const at::Tensor &t, int64_t &word) {
+        if (t.scalar_type() != type) {
+            PyErr_Format(PyExc_TypeError, "%s[%zd] must be %S", name, i, dtype);
+            return false;
+        }
+        if ((t.is_cuda() ? (int)t.get_device() : -1) != device) {
+            PyErr_Format(PyExc_ValueError, "%s[%zd]: all buffers must live on the same GPU", name, i);
+            return false;
+        }
+        if (!t.is_contiguous()) {
+            PyErr_Format(PyExc_ValueError, "%s[%zd]: buffers must be contiguous", name, i);
+            return false;
+        }
+        int64_t want = t.numel();
+        if (counted) std::memcpy(&want, PyBytes_AS_STRING(numels) + 8 * i, 8);
+        if (t.numel() != want) {
+            PyErr_Format(PyExc_ValueError, "%s[%zd] has %lld elements, not %lld", name, i, (long long)t.numel(),
+                         (long long)want);
+            return false;
+        }
+        word = (int64_t)(uintptr_t)t.const_data_ptr();
+        return true;
+    });
+}
+
+PyObject *numels(PyObject *, PyObject *list) {
+    return words(list, [](Py_ssize_t, const at::Tensor &t, int64_t &word) {
+        word = t.numel();
+        return true;
+    });
+}
+
+PyObject *rows(PyObject *, PyObject *args) {
+    const char *name;
+    PyObject *list;
+    Py_ssize_t columns;
+    if (!PyArg_ParseTuple(args, "sOn", &name, &list, &columns)) return nullptr;
+    return words(list, [&](Py_ssize_t i, const at::Tensor &t, int64_t &word) {
+        if (t.dim() != 2 || t.size(1) != columns) {
+            PyErr_Format(PyExc_ValueError, "%s[%zd] must have the shape [tokens, %zd]", name, i, columns);
+            return false;
+        }
+        word = t.size(0);
+        return true;
+    });
+}
+
+PyMethodDef methods[] = {{"read", (PyCFunction)read, METH_VARARGS, nullptr},
+                         {"numels", (PyCFunction)numels, METH_O, nullptr},
+                         {"rows", (PyCFunction)rows, METH_VARARGS, nullptr},
+                         {nullptr, nullptr, 0, nullptr}};
+PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
+
+}  // namespace
+
+PyMODINIT_FUNC PyInit__tensors() { return PyModule_Create(&module); }

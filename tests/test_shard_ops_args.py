@@ -81,6 +81,10 @@ def test_adamw_python():
         hc.adamw(p, [torch.zeros(5)], m, v, step=1, lr=0.1)
     with pytest.raises(ValueError, match="contiguous"):
         hc.adamw(p, [torch.zeros(8)[::2]], m, v, step=1, lr=0.1)
+    with pytest.raises(TypeError, match="tensors"):
+        hc.adamw(p, g, [None], v, step=1, lr=0.1)
+    with pytest.raises(ValueError, match="exp_avg_sqs has 2"):
+        hc.adamw(p, g, m, v * 2, step=1, lr=0.1)
     with pytest.raises(ValueError, match="scales of both"):
         hc.adamw(p, g, m, v, [torch.zeros(1)], step=1, lr=0.1)
     with pytest.raises(ValueError, match="bits"):
@@ -209,8 +213,14 @@ def test_balance_python():
         hc.balance_loss([], [], 4)
     with pytest.raises(TypeError, match="int32 or int64"):
         hc.balance_loss(x, [e[0].short()], 4)
-    with pytest.raises(ValueError, match="shape"):
+    with pytest.raises(ValueError, match="same tokens"):
         hc.balance_loss(x * 2, [e[0], e[0][:3]], 4)
+    with pytest.raises(ValueError, match=r"logits\[1\] must have the shape"):
+        hc.balance_loss([x[0], torch.zeros(4, 9)], e * 2, 4)
+    with pytest.raises(ValueError, match=r"experts\[1\] must have the shape"):
+        hc.balance_loss(x * 2, [e[0], e[0][0]], 4)
+    with pytest.raises(ValueError, match="contiguous"):
+        hc.balance_loss([torch.zeros(8, 4).t()], e, 4)
     with pytest.raises(ValueError, match="tokens"):
         hc.balance_loss([torch.zeros(4)], e, 4)
     with pytest.raises(ValueError, match="coef"):
