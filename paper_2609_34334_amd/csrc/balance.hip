@@ -85,7 +85,7 @@ struct Logits {
     static __device__ __forceinline__ int at(int j, int lane) { return (j * L + lane) * VE; }
     __device__ __forceinline__ void store(void *p, int lane, int E) const {
 #pragma unroll
-        for (int j = 0; j < NV; ++j) store_some<T>(p, at(j, lane), E, v[j]);
+        for (int j = 0; j < NV; ++j) store_some<T, true>(p, at(j, lane), E, v[j]);
     }
     // To exp(x - max) over the L lanes; returns what makes them p: the
     // reciprocal (1 ulp) of their sum.  Behind E there are zeros.
@@ -93,28 +93,51 @@ struct Logits {
         float top = -INFINITY, sum = 0.0f;
         if (E < L * N)
 #pragma unroll
-            for (int j = 0; j < NV; ++j)
+            for (int j = 0; j < NV; ++j) {
+                const int mine = here(E - at(j, lane));
 #pragma unroll
                 for (int i = 0; i < VE; ++i)
-                    if (at(j, lane) + i >= E) v[j][i] = -INFINITY;
+                    if (i >= mine) v[j][i] = -INFINITY;
+            }
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
             for (int i = 0; i < VE; ++i) top = fmaxf(top, v[j][i]);
         top = join_lanes<L, LaneMax>(top);
-        // All -inf: -inf - 0 leaves p = 0.
-        const float base = top == -INFINITY ? 0.0f : top;
+        if (fabsf(top) <= 1e38f) {
+            // In one step; the rounding of top log2 e is the same factor for
+            // all and goes with the sum.
+            const float base = -top * kLog2e;
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int i = 0; i < VE; ++i) v[j][i] = __builtin_amdgcn_exp2f(fmaf(v[j][i], kLog2e, base));
+        } else {
+            // All -inf: -inf - 0 leaves p = 0.  Others as large: the product
+            // with log2 e would overflow.
+            const float base = top == -INFINITY ? 0.0f : top;
+#pragma unroll
+            for (int j = 0; j < NV; ++j)
+#pragma unroll
+                for (int i = 0; i < VE; ++i) v[j][i] = __builtin_amdgcn_exp2f((v[j][i] - base) * kLog2e);
+        }
 #pragma unroll
         for (int j = 0; j < NV; ++j)
 #pragma unroll
-            for (int i = 0; i < VE; ++i) {
-                v[j][i] = __builtin_amdgcn_exp2f((v[j][i] - base) * kLog2e);
-                sum += v[j][i];
-            }
+            for (int i = 0; i < VE; ++i) sum += v[j][i];
         sum = join_lanes<L, LaneSum>(sum);
         return sum == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(sum);
     }
 };
+
+// Whether any of the L lanes of this lane's group has `v`.
+template <int L>
+__device__ __forceinline__ bool any_lane(bool v) {
+    const uint64_t all = __ballot(v);
+    if constexpr (L == 64) return all != 0;
+    const uint32_t lane = threadIdx.x % 64;
+    return (all >> (lane / L * L) & ((1ull << L % 64) - 1)) != 0;
+}
 
 // The batch of a block, and its place among the batch's blocks.
 __device__ __forceinline__ int batch_of(const BalanceArgs &a, uint32_t block, uint32_t &lb, uint32_t &nb) {
@@ -237,17 +260,18 @@ __global__ void __launch_bounds__(kThreads) balance_kernel(BalanceArgs) {
 // Loss, weights and counts of a batch from its blocks' sums.  The sums of p,
 // the counts of choices, of tokens a rank and of tokens are columns of one
 // table with a row a block; all are added in 64 bits, where the counts are
-// exact.  Lots of rows are added side by side, four columns a thread and eight
+// exact.  Lots of rows are added side by side, four columns a thread and twelve
 // rows of them in flight, then the lots in order: one row and column after
 // another, 64 blocks took 35 us, all latency; a column a thread 11 (256
 // experts).
 constexpr int kFinishThreads = 1024;
+constexpr int kLotAhead = 12;
 constexpr int kColumns = 2 * kMaxExperts + 64 + 4;
 __global__ void __launch_bounds__(kFinishThreads) balance_finish_kernel(BalanceArgs) {
     const BalanceArgs &a = kernel_args<BalanceArgs>();
     __shared__ double lot[kFinishThreads][4];
     __shared__ double tot[kColumns];
-    __shared__ double rank_choices[64];
+    __shared__ int rank_choices[64];
     __shared__ double red[kFinishThreads / 64][2];
     const int E = a.E, D = a.D, per = E / D, cols = balance_columns(E, D), t = threadIdx.x;
     const int wide = cols / 4, lots = kFinishThreads / wide, g = t / wide, c = t % wide * 4;
@@ -256,16 +280,16 @@ __global__ void __launch_bounds__(kFinishThreads) balance_finish_kernel(BalanceA
         const int32_t *rows = a.partial + (uint64_t)a.first[seg] * cols + c;
         if (g < lots) {
             double sum[4] = {};
-            for (uint32_t b0 = g; b0 < nb; b0 += 8 * lots) {
-                Raw<16> v[8];
+            for (uint32_t b0 = g; b0 < nb; b0 += kLotAhead * lots) {
+                Raw<16> v[kLotAhead];
 #pragma unroll
-                for (int i = 0; i < 8; ++i) {
+                for (int i = 0; i < kLotAhead; ++i) {
                     const uint32_t b = b0 + i * lots;
                     if (b < nb) load_raw(v[i], rows + (uint64_t)b * cols);
                     else v[i] = {};
                 }
 #pragma unroll
-                for (int i = 0; i < 8; ++i)
+                for (int i = 0; i < kLotAhead; ++i)
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
                         sum[j] += c + j < E ? (double)__uint_as_float(v[i].w[j]) : (double)(int32_t)v[i].w[j];
@@ -276,6 +300,7 @@ __global__ void __launch_bounds__(kFinishThreads) balance_finish_kernel(BalanceA
         __syncthreads();
         for (int i = t; i < cols; i += kFinishThreads) {
             double sum = 0.0;
+#pragma unroll 8
             for (int l = 0; l < lots; ++l) sum += lot[l * wide + i / 4][i % 4];
             tot[i] = sum;
         }
@@ -283,33 +308,27 @@ __global__ void __launch_bounds__(kFinishThreads) balance_finish_kernel(BalanceA
         for (int e = t; e < E; e += kFinishThreads) a.expert_tokens[(uint64_t)seg * E + e] = (int32_t)tot[E + e];
         if (t < D) a.rank_tokens[(uint64_t)seg * D + t] = (int32_t)tot[2 * E + t];
         for (int d = t / 64; d < D; d += kFinishThreads / 64) {  // a wave a rank
-            double n = 0.0;
-            for (int e = d * per + t % 64; e < (d + 1) * per; e += 64) n += tot[E + e];
-#pragma unroll
-            for (int o = 32; o > 0; o /= 2) n += __shfl_xor(n, o);
+            int n = 0;
+            for (int e = d * per + t % 64; e < (d + 1) * per; e += 64) n += (int)tot[E + e];
+            n = join_lanes<64, LaneSum>(n);
             if (t % 64 == 0) rank_choices[d] = n;
         }
         __syncthreads();
-        const double live = tot[2 * E + D], T = live > 0.0 ? live : 1.0;
+        const double live = tot[2 * E + D], over = live > 0.0 ? 1.0 / live : 0.0;
         double loss = 0.0, all = 0.0, w = 0.0;
         if (t < E) {
             const int d = t / per;
-            const double f = (double)E / ((double)a.k * T);
-            w = a.expert_weight * f * tot[E + t] + a.rank_weight * f * rank_choices[d] / per +
-                a.traffic_weight * (double)D * tot[2 * E + d] / ((double)a.max_ranks * T);
-            loss = w * tot[t] / T;
+            w = (a.expert_scale * tot[E + t] + a.rank_scale * rank_choices[d] + a.traffic_scale * tot[2 * E + d]) * over;
+            loss = w * tot[t] * over;
             all = w;
         }
-#pragma unroll
-        for (int o = 32; o > 0; o /= 2) {
-            loss += __shfl_xor(loss, o);
-            all += __shfl_xor(all, o);
-        }
+        loss = join_lanes<64, LaneSum>(loss);
+        all = join_lanes<64, LaneSum>(all);
         if (t % 64 == 0) red[t / 64][0] = loss, red[t / 64][1] = all;
         __syncthreads();
         loss = 0.0, all = 0.0;
         for (int i = 0; i < (E + 63) / 64; ++i) loss += red[i][0], all += red[i][1];
-        if (t < E) a.coef[(uint64_t)seg * E + t] = live > 0.0 ? (float)((w - all / E) / T) : 0.0f;
+        if (t < E) a.coef[(uint64_t)seg * E + t] = (float)((w - all / E) * over);
         if (t == 0) a.loss[seg] = (float)loss;
         __syncthreads();
     }
@@ -350,23 +369,25 @@ __global__ void __launch_bounds__(kOpThreads) balance_backward_kernel(BalanceArg
                 const uint32_t row = u * ROWS + slot;
                 const bool in = row < left;
                 for (int c = lane + L; c < k; c += L) any[u] |= in && choice(a, experts, row * k + c) >= 0;
-                const bool valid = join_lanes<L, LaneOr>((uint32_t)any[u]) != 0;
                 X x(now[u]);
-                const float inv = x.softmax(lane, E);
-                float dot = 0.0f;
+                if (any_lane<L>(any[u])) {
+                    const float inv = x.softmax(lane, E), scale = g * inv;
+                    float dot = 0.0f;
 #pragma unroll
-                for (int j = 0; j < X::NV; ++j)
+                    for (int j = 0; j < X::NV; ++j)
 #pragma unroll
-                    for (int i = 0; i < X::VE; ++i) {
-                        x.v[j][i] *= inv;
-                        dot += x.v[j][i] * w[j][i];
-                    }
-                dot = join_lanes<L, LaneSum>(dot);
+                        for (int i = 0; i < X::VE; ++i) dot += x.v[j][i] * w[j][i];
+                    const float mean = join_lanes<L, LaneSum>(dot) * inv * scale;
 #pragma unroll
-                for (int j = 0; j < X::NV; ++j)
+                    for (int j = 0; j < X::NV; ++j)
 #pragma unroll
-                    for (int i = 0; i < X::VE; ++i)
-                        x.v[j][i] = valid ? g * x.v[j][i] * (w[j][i] - dot) : 0.0f;
+                        for (int i = 0; i < X::VE; ++i) x.v[j][i] *= fmaf(w[j][i], scale, -mean);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < X::NV; ++j)
+#pragma unroll
+                        for (int i = 0; i < X::VE; ++i) x.v[j][i] = 0.0f;
+                }
                 x.store(dlogits + row * (uint32_t)E * T::size, lane, in ? E : 0);
             }
         }

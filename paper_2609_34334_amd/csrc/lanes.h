@@ -93,20 +93,35 @@ struct EBF16 {
     }
     template <int N>
     static __device__ __forceinline__ void pack(const float (&f)[N], Raw<2 * N> &r) {
+        typedef float f2 __attribute__((ext_vector_type(2)));
+        typedef __bf16 b2 __attribute__((ext_vector_type(2)));
 #pragma unroll
-        for (int i = 0; i < N / 2; ++i)
-            r.w[i] = (uint32_t)narrow(f[2 * i]) | ((uint32_t)narrow(f[2 * i + 1]) << 16);
+        for (int i = 0; i < N / 2; ++i) {  // one instruction converts and packs two
+            const f2 x = {f[2 * i], f[2 * i + 1]};
+            r.w[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, b2));
+        }
     }
 };
 
+// The same value, which the compiler takes for another.  The element-by-element
+// ends below start with it, so that their comparisons stay there: hoisted out
+// of the callers' loops they took a dozen registers and as many instructions
+// of every pass.
+template <typename V>
+__device__ __forceinline__ V here(V v) {
+    asm volatile("" : "+v"(v));
+    return v;
+}
+
 // A vector of 16 bytes of `p` from element e on; elements at and behind `end`
 // are zeros and are not read.
-template <class T, typename I>
+template <class T, bool NT = false, typename I>
 __device__ __forceinline__ void load_vector(const void *p, I e, I end, Raw<16> &r) {
     constexpr int N = 16 / T::size;
     if (e + N <= end) {
-        load_raw(r, (const char *)p + (size_t)e * T::size);
+        load_raw<NT>(r, (const char *)p + (size_t)e * T::size);
     } else {
+        e = here(e);
 #pragma unroll
         for (int i = 0; i < 4; ++i) r.w[i] = 0;
 #pragma unroll
@@ -127,6 +142,7 @@ __device__ __forceinline__ void load_some(const void *p, I e, I end, float (&f)[
         load_raw<NT>(r, (const char *)p + (size_t)e * T::size);
         T::template unpack<N>(r, f);
     } else {
+        e = here(e);
 #pragma unroll
         for (int i = 0; i < N; ++i) f[i] = e + i < end ? T::widen(((const typename T::S *)p)[e + i]) : 0.0f;
     }
@@ -139,6 +155,7 @@ __device__ __forceinline__ void store_some(void *p, I e, I end, const float (&f)
         T::template pack<N>(f, r);
         store_raw<NT>((char *)p + e * T::size, r);
     } else {
+        e = here(e);
 #pragma unroll
         for (int i = 0; i < N; ++i)
             if (e + i < end) ((typename T::S *)p)[e + i] = T::narrow(f[i]);
@@ -148,7 +165,8 @@ __device__ __forceinline__ void store_some(void *p, I e, I end, const float (&f)
 // ---- lanes -------------------------------------------------------------------
 
 struct LaneSum {
-    static __device__ __forceinline__ float join(float a, float b) { return a + b; }
+    template <typename V>
+    static __device__ __forceinline__ V join(V a, V b) { return a + b; }
 };
 struct LaneMax {  // NaN gives way to a number
     static __device__ __forceinline__ float join(float a, float b) { return fmaxf(a, b); }
@@ -168,6 +186,41 @@ template <int CTRL>
 __device__ __forceinline__ float dpp(float v) {
     return __uint_as_float(dpp<CTRL>(__float_as_uint(v)));
 }
+template <int CTRL>
+__device__ __forceinline__ int dpp(int v) {
+    return (int)dpp<CTRL>((uint32_t)v);
+}
+struct U2 {
+    uint32_t a, b;
+};
+template <int CTRL>
+__device__ __forceinline__ double dpp(double v) {
+    const U2 x = __builtin_bit_cast(U2, v);
+    return __builtin_bit_cast(double, U2{dpp<CTRL>(x.a), dpp<CTRL>(x.b)});
+}
+
+// v of the other row of 16 (SWAP32: of the other half of the wave) joined
+// with the lane's own.
+template <bool SWAP32>
+__device__ __forceinline__ U2 swap_rows(uint32_t v) {
+    if constexpr (SWAP32) {
+        const auto r = __builtin_amdgcn_permlane32_swap(v, v, false, false);
+        return {r[0], r[1]};
+    } else {
+        const auto r = __builtin_amdgcn_permlane16_swap(v, v, false, false);
+        return {r[0], r[1]};
+    }
+}
+template <bool SWAP32, class J, typename V>
+__device__ __forceinline__ V join_rows(V v) {
+    if constexpr (sizeof(V) == 8) {
+        const U2 x = __builtin_bit_cast(U2, v), lo = swap_rows<SWAP32>(x.a), hi = swap_rows<SWAP32>(x.b);
+        return J::join(__builtin_bit_cast(V, U2{lo.a, hi.a}), __builtin_bit_cast(V, U2{lo.b, hi.b}));
+    } else {
+        const U2 r = swap_rows<SWAP32>(__builtin_bit_cast(uint32_t, v));
+        return J::join(__builtin_bit_cast(V, r.a), __builtin_bit_cast(V, r.b));
+    }
+}
 
 // v of every lane joined over each aligned group of L lanes (a power of two
 // up to 64), the result in all of them.  A group's lanes take part together;
@@ -181,17 +234,8 @@ __device__ __forceinline__ V join_lanes(V v) {
     if constexpr (L >= 4) v = J::join(v, dpp<0x4E>(v));    // quad_perm 2,3,0,1
     if constexpr (L >= 8) v = J::join(v, dpp<0x141>(v));   // row_half_mirror
     if constexpr (L >= 16) v = J::join(v, dpp<0x140>(v));  // row_mirror
-    auto bits = [](V x) { return __builtin_bit_cast(uint32_t, x); };
-    if constexpr (L >= 32) {
-        const auto r = __builtin_amdgcn_permlane16_swap(bits(v), bits(v), false, false);
-        const uint32_t a = r[0], b = r[1];  // a bit_cast of r[1] itself takes r[0]
-        v = J::join(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b));
-    }
-    if constexpr (L >= 64) {
-        const auto r = __builtin_amdgcn_permlane32_swap(bits(v), bits(v), false, false);
-        const uint32_t a = r[0], b = r[1];  // a bit_cast of r[1] itself takes r[0]
-        v = J::join(__builtin_bit_cast(V, a), __builtin_bit_cast(V, b));
-    }
+    if constexpr (L >= 32) v = join_rows<false, J>(v);
+    if constexpr (L >= 64) v = join_rows<true, J>(v);
     return v;
 }
 
@@ -245,6 +289,7 @@ __device__ __forceinline__ void load_bytes(const void *p, I e, I end, Raw<N> &r)
     if (e + N <= end) {
         load_raw<NT>(r, (const char *)p + e);
     } else {
+        e = here(e);
 #pragma unroll
         for (int i = 0; i < N / 4; ++i) r.w[i] = 0;
 #pragma unroll
@@ -257,6 +302,7 @@ __device__ __forceinline__ void store_bytes(void *p, I e, I end, const Raw<N> &r
     if (e + N <= end) {
         store_raw<NT>((char *)p + e, r);
     } else {
+        e = here(e);
 #pragma unroll
         for (int i = 0; i < N; ++i)
             if (e + i < end) ((uint8_t *)p)[e + i] = (uint8_t)(r.w[i / 4] >> (8 * (i % 4)));

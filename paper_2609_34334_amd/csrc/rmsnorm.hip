@@ -25,6 +25,11 @@
 // 46, 17 and 104.  Sums are in fp32, in an order that goes by the row's length
 // alone.
 //
+// The backward pass reads and writes past the caches (105 us otherwise, 94 so,
+// at 16384 x 4096); the forward pass writes past them (4096 x 2048 into 8 bits
+// 12.5 and 11.5 us, 8192 x 4096 50.8 and 50.0) but reads through them, as its
+// inputs have mostly just been made (read past them 12.8 and 48.5).
+//
 // Bound by memory: 8 bytes an element (bf16 with a residual), 7 with y in 8
 // bits; backward 8 bytes and the partial sums of the weight's gradient.
 #include <algorithm>
@@ -56,10 +61,11 @@ struct Shaped {
     static constexpr bool ahead = N <= 8, keep_weights = N <= 16;
     Raw<16> v[NV];
     // W threads a row, of which this is number t.
+    template <bool NT>
     __device__ __forceinline__ void load(const void *p, uint64_t row, uint32_t H, uint32_t W, uint32_t t) {
         const char *at = (const char *)p + row * H * T::size;
 #pragma unroll
-        for (int j = 0; j < NV; ++j) load_vector<T>(at, (j * W + t) * VE, H, v[j]);
+        for (int j = 0; j < NV; ++j) load_vector<T, NT>(at, (j * W + t) * VE, H, v[j]);
     }
     __device__ __forceinline__ void unpack(int j, float (&f)[VE]) const { T::template unpack<VE>(v[j], f); }
     // The same values, which the compiler takes for others: what it unpacked
@@ -104,8 +110,8 @@ __global__ void __launch_bounds__(WAVE ? kOpThreads : 1024) rmsnorm_kernel(const
     uint64_t row = (uint64_t)blockIdx.x * ROWS + (WAVE ? threadIdx.x / 64 : 0);
     X x, res;
     auto load = [&](uint64_t r) {
-        x.load(a.x, r, H, W, t);
-        if (a.residual) res.load(a.residual, r, H, W, t);
+        x.template load<false>(a.x, r, H, W, t);
+        if (a.residual) res.template load<false>(a.residual, r, H, W, t);
     };
     if (X::ahead && row < a.rows) load(row);
     float w[NV][VE];
@@ -129,7 +135,7 @@ __global__ void __launch_bounds__(WAVE ? kOpThreads : 1024) rmsnorm_kernel(const
         if (X::ahead && row + step < a.rows) load(row + step);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            if (a.residual_out) store_some<T>((char *)a.residual_out + at, (j * W + t) * VE, H, h[j]);
+            if (a.residual_out) store_some<T, true>((char *)a.residual_out + at, (j * W + t) * VE, H, h[j]);
 #pragma unroll
             for (int i = 0; i < VE; ++i) sum[0] += h[j][i] * h[j][i];
         }
@@ -153,10 +159,10 @@ __global__ void __launch_bounds__(WAVE ? kOpThreads : 1024) rmsnorm_kernel(const
                 for (int i = 0; i < VE; ++i) y[i] *= inverse;
                 Raw<VE> q;
                 to_e4m3(y, q);
-                store_bytes((char *)a.y + row * H, e, H, q);
+                store_bytes<true>((char *)a.y + row * H, e, H, q);
                 if (e % kBlock == 0 && e < H) a.scale[row * nblk + e / kBlock] = scale;
             } else {
-                store_some<T>((char *)a.y + at, e, H, y);
+                store_some<T, true>((char *)a.y + at, e, H, y);
             }
         }
     }
@@ -177,9 +183,9 @@ __global__ void __launch_bounds__(WAVE ? kOpThreads : 1024) rmsnorm_backward_ker
     const uint64_t step = (uint64_t)a.blocks * ROWS;
     X h, g, d;
     auto load = [&](uint64_t r) {
-        h.load(a.h, r, H, W, t);
-        g.load(a.dy, r, H, W, t);
-        if (a.dres) d.load(a.dres, r, H, W, t);
+        h.template load<true>(a.h, r, H, W, t);
+        g.template load<true>(a.dy, r, H, W, t);
+        if (a.dres) d.template load<true>(a.dres, r, H, W, t);
     };
     float w[NV][VE];
     if (X::keep_weights)
@@ -222,7 +228,7 @@ __global__ void __launch_bounds__(WAVE ? kOpThreads : 1024) rmsnorm_backward_ker
                     x[i] += r * (y[i] * w[j][i] - u[i] * c);
                     dw[j][i] += y[i] * (u[i] * r);
                 }
-                store_some<T>((char *)a.dx + row * H * T::size, (j * W + t) * VE, H, x);
+                store_some<T, true>((char *)a.dx + row * H * T::size, (j * W + t) * VE, H, x);
             }
         }
         if (!a.partial) continue;

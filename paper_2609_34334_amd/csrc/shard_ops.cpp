@@ -304,8 +304,10 @@ hoccl_status_t fill_balance(const hoccl_balance_t &o, const void *const *logits,
     // than 2^10, which keeps e / experts-of-a-rank exact below 1024.
     const uint32_t per = (uint32_t)(o.experts / o.ranks);
     a.rank_mul = ((1u << 21) + per - 1) / per;
-    a.expert_weight = o.expert_weight, a.rank_weight = o.rank_weight, a.traffic_weight = o.traffic_weight;
-    a.max_ranks = o.max_ranks > 0 ? o.max_ranks : std::min(o.topk, o.ranks);
+    const int max_ranks = o.max_ranks > 0 ? o.max_ranks : std::min(o.topk, o.ranks);
+    a.expert_scale = o.expert_weight * o.experts / o.topk;
+    a.rank_scale = o.rank_weight * o.experts / ((double)o.topk * per);
+    a.traffic_scale = o.traffic_weight * o.ranks / max_ranks;
     return HOCCL_OK;
 }
 

@@ -108,8 +108,9 @@ struct BalanceArgs {
     int32_t *expert_tokens, *rank_tokens;  // [nseg][E], [nseg][D]
     float *coef;           // [nseg][E]
     const float *grad;     // [nseg] or null
-    double expert_weight, rank_weight, traffic_weight;
-    int max_ranks;
+    // w times the tokens: of a choice, of a choice of the rank's, of a token
+    // that goes to the rank.
+    double expert_scale, rank_scale, traffic_scale;
 };
 
 // Words of a block's sums: E of p, E + D + 1 counts, and up to four's multiple.
