@@ -46,6 +46,10 @@ constexpr int kAhead = 2;      // tokens of a lane in flight
 // passes as the others, whatever the batches' lengths (eight batches of 9,800
 // to 32,768 tokens, 256 experts: 51 us with as many workgroups for each).
 constexpr size_t kBlocks = 512;
+// Batches of no more passes than this are a workgroup's each, which finishes
+// its batch without a second kernel: 256 tokens and 64 experts take 7.1 us
+// instead of 8.9, but 512 tokens, four passes, 10.0 instead of 8.9.
+constexpr size_t kOnePasses = 2;
 constexpr float kLog2e = 1.4426950408889634f;
 
 int lanes_of(int E) {
@@ -62,6 +66,22 @@ __device__ __forceinline__ int choice(const BalanceArgs &a, const char *experts,
     }
     const uint32_t v = ((const uint32_t *)experts)[i];
     return v < (uint32_t)a.E ? (int)v : -1;
+}
+
+// f(choice) of a lane's choices but the first of a token whose `k` choices
+// start at `at`: eight reads at once, since one after another each would wait
+// for memory.
+template <int L, class F>
+__device__ __forceinline__ void more_choices(const BalanceArgs &a, const char *experts, uint32_t at, int lane, int k,
+                                             F &&f) {
+    constexpr int AHEAD = 8;
+    for (int c = lane + L; c < k; c += AHEAD * L) {
+        int e[AHEAD];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) e[i] = c + i * L < k ? choice(a, experts, at + c + i * L) : -1;
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) f(e[i]);
+    }
 }
 
 // A lane's logits of one token: NV vectors of VE, L lanes apart.
@@ -147,22 +167,73 @@ __device__ __forceinline__ int batch_of(const BalanceArgs &a, uint32_t block, ui
     return seg;
 }
 
-template <class T, int L, int N>
+// Loss, weights and counts of a batch from its sums: the table's columns, in
+// 64 bits.  For all threads of a workgroup of NT.
+template <int NT>
+__device__ __forceinline__ void finish_batch(const BalanceArgs &a, int seg, const double *tot) {
+    constexpr int OWN = (kMaxExperts + NT - 1) / NT;  // experts of a thread
+    __shared__ int rank_choices[64];
+    __shared__ double red[NT / 64][2];
+    const int E = a.E, D = a.D, per = E / D, t = threadIdx.x;
+    for (int e = t; e < E; e += NT) a.expert_tokens[(uint64_t)seg * E + e] = (int32_t)tot[E + e];
+    if (t < D) a.rank_tokens[(uint64_t)seg * D + t] = (int32_t)tot[2 * E + t];
+    for (int d = t / 64; d < D; d += NT / 64) {  // a wave a rank
+        int n = 0;
+        for (int e = d * per + t % 64; e < (d + 1) * per; e += 64) n += (int)tot[E + e];
+        n = join_lanes<64, LaneSum>(n);
+        if (t % 64 == 0) rank_choices[d] = n;
+    }
+    __syncthreads();
+    const double live = tot[2 * E + D], over = live > 0.0 ? 1.0 / live : 0.0;
+    double loss = 0.0, all = 0.0, w[OWN] = {};
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) {
+        const int e = i * NT + t;
+        if (e >= E) continue;
+        const int d = (int)(((uint32_t)e * a.rank_mul) >> 21);
+        w[i] = (a.expert_scale * tot[E + e] + a.rank_scale * rank_choices[d] + a.traffic_scale * tot[2 * E + d]) * over;
+        loss += w[i] * tot[e] * over;
+        all += w[i];
+    }
+    loss = join_lanes<64, LaneSum>(loss);
+    all = join_lanes<64, LaneSum>(all);
+    if (t % 64 == 0) red[t / 64][0] = loss, red[t / 64][1] = all;
+    __syncthreads();
+    loss = 0.0, all = 0.0;
+    for (int i = 0; i < min((E + 63) / 64, NT / 64); ++i) loss += red[i][0], all += red[i][1];
+#pragma unroll
+    for (int i = 0; i < OWN; ++i) {
+        const int e = i * NT + t;
+        if (e < E) a.coef[(uint64_t)seg * E + e] = (float)((w[i] - all / E) * over);
+    }
+    if (t == 0) a.loss[seg] = (float)loss;
+    __syncthreads();
+}
+
+constexpr int kColumns = 2 * kMaxExperts + 64 + 4;
+
+// ONE: every batch is one workgroup's, which finishes it.
+template <class T, int L, int N, bool ONE>
 __global__ void __launch_bounds__(kThreads) balance_kernel(BalanceArgs) {
     const BalanceArgs &a = kernel_args<BalanceArgs>();
     using X = Logits<T, L, N>;
     constexpr int ROWS = kThreads / L;     // tokens of a workgroup's pass, kAhead times
     constexpr int OWN = L < 8 ? 8 : 64 / L;  // ranks a lane counts: no more than its experts, nor 64 in all
     __shared__ float sum_p[kWaves][L * N];
-    __shared__ int sum_n[L * N];
+    // Choices, a copy for each of a wave's groups, so that the 64 lanes that
+    // hold tokens of 8 experts do not meet at eight addresses.
+    constexpr int COPIES = 64 / L;
+    __shared__ int sum_n[L * N * COPIES];
     __shared__ int sum_sent[64];
     __shared__ int sum_live;
+    __shared__ double tot[ONE ? kColumns : 1];
     const int E = a.E, D = a.D, k = a.k, stride = balance_columns(E, D);
     const int lane = threadIdx.x % L, slot = threadIdx.x / L;
     for (uint32_t block = blockIdx.x; block < a.first[a.nseg]; block += gridDim.x) {
         uint32_t lb, nb;
-        const BalanceSeg &s = a.seg[batch_of(a, block, lb, nb)];
-        for (int e = threadIdx.x; e < E; e += kThreads) sum_n[e] = 0;
+        const int seg = batch_of(a, block, lb, nb);
+        const BalanceSeg &s = a.seg[seg];
+        for (int e = threadIdx.x; e < E * COPIES; e += kThreads) sum_n[e] = 0;
         if (threadIdx.x < 64) sum_sent[threadIdx.x] = 0;
         if (threadIdx.x == 0) sum_live = 0;
         __syncthreads();
@@ -204,11 +275,10 @@ __global__ void __launch_bounds__(kThreads) balance_kernel(BalanceArgs) {
                     const uint32_t d = ((uint32_t)e * a.rank_mul) >> 21;
                     if (d < 32) lo |= 1u << d;
                     else hi |= 1u << (d - 32);
-                    atomicAdd(&sum_n[e], 1);
+                    atomicAdd(&sum_n[e * COPIES + slot % COPIES], 1);
                 };
                 choose(first[u]);
-                for (int c = lane + L; c < k; c += L)
-                    if (row < left) choose(choice(a, experts, row * k + c));
+                more_choices<L>(a, experts, row * k, lane, row < left ? k : 0, choose);
                 lo = join_lanes<L, LaneOr>(lo);
                 if (D > 32) hi = join_lanes<L, LaneOr>(hi);
                 if ((lo | hi) == 0) continue;  // padding, for all of the token's lanes
@@ -226,54 +296,60 @@ __global__ void __launch_bounds__(kThreads) balance_kernel(BalanceArgs) {
                     for (int i = 0; i < X::VE; ++i) acc[j][i] += x.v[j][i] * inv;
             }
         }
-        // The wave's groups, then the waves in order.
+        // The wave's groups, then the waves: sums of p in order.
 #pragma unroll
-        for (int o = L; o < 64; o *= 2)
+        for (int j = 0; j < X::NV; ++j)
 #pragma unroll
-            for (int j = 0; j < X::NV; ++j)
+            for (int i = 0; i < X::VE; ++i) acc[j][i] = join_groups<L, LaneSum>(acc[j][i]);
 #pragma unroll
-                for (int i = 0; i < X::VE; ++i) acc[j][i] += __shfl_xor(acc[j][i], o);
-        if (threadIdx.x % 64 < L)
+        for (int i = 0; i < OWN; ++i) sent[i] = join_groups<L, LaneSum>(sent[i]);
+        live = join_groups<L, LaneSum>(live);
+        if (threadIdx.x % 64 < L) {
 #pragma unroll
             for (int j = 0; j < X::NV; ++j)
 #pragma unroll
                 for (int i = 0; i < X::VE; ++i) sum_p[threadIdx.x / 64][X::at(j, lane) + i] = acc[j][i];
 #pragma unroll
-        for (int i = 0; i < OWN; ++i)
-            if (sent[i]) atomicAdd(&sum_sent[i * L + lane], sent[i]);
-        if (live) atomicAdd(&sum_live, live);
+            for (int i = 0; i < OWN; ++i)
+                if (sent[i]) atomicAdd(&sum_sent[i * L + lane], sent[i]);
+            if (live) atomicAdd(&sum_live, live);
+        }
         __syncthreads();
         int32_t *out = a.partial + (uint64_t)block * stride;
         for (int e = threadIdx.x; e < E; e += kThreads) {
             float p = 0.0f;
+            int n = 0;
 #pragma unroll
             for (int w = 0; w < kWaves; ++w) p += sum_p[w][e];
-            out[e] = __float_as_int(p);
-            out[E + e] = sum_n[e];
+#pragma unroll 8
+            for (int c = 0; c < COPIES; ++c) n += sum_n[e * COPIES + c];
+            if constexpr (ONE) tot[e] = p, tot[E + e] = n;
+            else out[e] = __float_as_int(p), out[E + e] = n;
         }
-        if ((int)threadIdx.x < D) out[2 * E + threadIdx.x] = sum_sent[threadIdx.x];
-        if (threadIdx.x == 0) out[2 * E + D] = sum_live;
-        __syncthreads();
+        if constexpr (ONE) {
+            if ((int)threadIdx.x < D) tot[2 * E + threadIdx.x] = sum_sent[threadIdx.x];
+            if (threadIdx.x == 0) tot[2 * E + D] = sum_live;
+            __syncthreads();
+            finish_batch<kThreads>(a, seg, tot);
+        } else {
+            if ((int)threadIdx.x < D) out[2 * E + threadIdx.x] = sum_sent[threadIdx.x];
+            if (threadIdx.x == 0) out[2 * E + D] = sum_live;
+            __syncthreads();
+        }
     }
 }
 
-// Loss, weights and counts of a batch from its blocks' sums.  The sums of p,
-// the counts of choices, of tokens a rank and of tokens are columns of one
-// table with a row a block; all are added in 64 bits, where the counts are
-// exact.  Lots of rows are added side by side, four columns a thread and twelve
-// rows of them in flight, then the lots in order: one row and column after
-// another, 64 blocks took 35 us, all latency; a column a thread 11 (256
-// experts).
+// The same from the sums of a batch's blocks, rows of the table.  Lots of rows
+// are added side by side, four columns a thread and twelve rows of them in
+// flight, then the lots in order: one row and column after another, 64 blocks
+// took 35 us, all latency; a column a thread 11 (256 experts), so 8.
 constexpr int kFinishThreads = 1024;
 constexpr int kLotAhead = 12;
-constexpr int kColumns = 2 * kMaxExperts + 64 + 4;
 __global__ void __launch_bounds__(kFinishThreads) balance_finish_kernel(BalanceArgs) {
     const BalanceArgs &a = kernel_args<BalanceArgs>();
     __shared__ double lot[kFinishThreads][4];
     __shared__ double tot[kColumns];
-    __shared__ int rank_choices[64];
-    __shared__ double red[kFinishThreads / 64][2];
-    const int E = a.E, D = a.D, per = E / D, cols = balance_columns(E, D), t = threadIdx.x;
+    const int E = a.E, cols = balance_columns(E, a.D), t = threadIdx.x;
     const int wide = cols / 4, lots = kFinishThreads / wide, g = t / wide, c = t % wide * 4;
     for (int seg = blockIdx.x; seg < a.nseg; seg += gridDim.x) {
         const uint32_t nb = a.first[seg + 1] - a.first[seg];
@@ -305,35 +381,9 @@ __global__ void __launch_bounds__(kFinishThreads) balance_finish_kernel(BalanceA
             tot[i] = sum;
         }
         __syncthreads();
-        for (int e = t; e < E; e += kFinishThreads) a.expert_tokens[(uint64_t)seg * E + e] = (int32_t)tot[E + e];
-        if (t < D) a.rank_tokens[(uint64_t)seg * D + t] = (int32_t)tot[2 * E + t];
-        for (int d = t / 64; d < D; d += kFinishThreads / 64) {  // a wave a rank
-            int n = 0;
-            for (int e = d * per + t % 64; e < (d + 1) * per; e += 64) n += (int)tot[E + e];
-            n = join_lanes<64, LaneSum>(n);
-            if (t % 64 == 0) rank_choices[d] = n;
-        }
-        __syncthreads();
-        const double live = tot[2 * E + D], over = live > 0.0 ? 1.0 / live : 0.0;
-        double loss = 0.0, all = 0.0, w = 0.0;
-        if (t < E) {
-            const int d = t / per;
-            w = (a.expert_scale * tot[E + t] + a.rank_scale * rank_choices[d] + a.traffic_scale * tot[2 * E + d]) * over;
-            loss = w * tot[t] * over;
-            all = w;
-        }
-        loss = join_lanes<64, LaneSum>(loss);
-        all = join_lanes<64, LaneSum>(all);
-        if (t % 64 == 0) red[t / 64][0] = loss, red[t / 64][1] = all;
-        __syncthreads();
-        loss = 0.0, all = 0.0;
-        for (int i = 0; i < (E + 63) / 64; ++i) loss += red[i][0], all += red[i][1];
-        if (t < E) a.coef[(uint64_t)seg * E + t] = (float)((w - all / E) * over);
-        if (t == 0) a.loss[seg] = (float)loss;
-        __syncthreads();
+        finish_batch<kFinishThreads>(a, seg, tot);
     }
 }
-static_assert(kMaxExperts <= kFinishThreads, "a thread an expert");
 
 template <class T, int L, int N>
 __global__ void __launch_bounds__(kOpThreads) balance_backward_kernel(BalanceArgs) {
@@ -368,7 +418,7 @@ __global__ void __launch_bounds__(kOpThreads) balance_backward_kernel(BalanceArg
             for (int u = 0; u < kAhead; ++u) {
                 const uint32_t row = u * ROWS + slot;
                 const bool in = row < left;
-                for (int c = lane + L; c < k; c += L) any[u] |= in && choice(a, experts, row * k + c) >= 0;
+                more_choices<L>(a, experts, row * k, lane, in ? k : 0, [&](int e) { any[u] |= e >= 0; });
                 X x(now[u]);
                 if (any_lane<L>(any[u])) {
                     const float inv = x.softmax(lane, E), scale = g * inv;
@@ -421,15 +471,22 @@ void balance_blocks(const size_t *tokens, int E, int batches, uint32_t *first) {
     const size_t rows = rows_of(E, kThreads);
     size_t all = 0, longest = 0;
     for (int b = 0; b < batches; ++b) all += over(tokens[b], rows), longest = std::max(longest, tokens[b]);
-    const size_t passes = std::max({(size_t)1, over(all, kBlocks), over(over(longest, rows), kBlocks / 2)});
     first[0] = 0;
+    if (longest <= rows * kOnePasses) {
+        for (int b = 0; b < batches; ++b) first[b + 1] = (uint32_t)(b + 1);
+        return;
+    }
+    const size_t passes = std::max({(size_t)1, over(all, kBlocks), over(over(longest, rows), kBlocks / 2)});
     for (int b = 0; b < batches; ++b)
         first[b + 1] = first[b] + (uint32_t)std::max((size_t)1, over(tokens[b], rows * passes));
 }
 
 hipError_t launch_balance(const BalanceArgs &a, hoccl_dtype_t dt, int wg, hipStream_t s) {
-    const void *k = with_lanes(dt, a.E, [](auto t, auto l, auto n) {
-        return (const void *)balance_kernel<decltype(t), decltype(l)::value, decltype(n)::value>;
+    const bool one = balance_is_one(a);
+    const void *k = with_lanes(dt, a.E, [&](auto t, auto l, auto n) {
+        constexpr int L = decltype(l)::value, N = decltype(n)::value;
+        return one ? (const void *)balance_kernel<decltype(t), L, N, true>
+                   : (const void *)balance_kernel<decltype(t), L, N, false>;
     });
     void *args[] = {(void *)&a};
     return hipLaunchKernel(k, dim3((unsigned)wg), dim3(kThreads), args, 0, s);

@@ -239,6 +239,18 @@ __device__ __forceinline__ V join_lanes(V v) {
     return v;
 }
 
+// The other way round: v joined over the wave's lanes that have the same place
+// in their groups of L.  For whole waves.
+template <int L, class J, typename V>
+__device__ __forceinline__ V join_groups(V v) {
+#pragma unroll
+    for (int o = L; o < 8; o *= 2) v = J::join(v, (V)__shfl_xor(v, o));
+    if constexpr (L <= 8) v = J::join(v, dpp<0x128>(v));  // row_ror:8
+    if constexpr (L <= 16) v = join_rows<false, J>(v);
+    if constexpr (L <= 32) v = join_rows<true, J>(v);
+    return v;
+}
+
 // ---- 8 bits: e4m3 with one fp32 scale for each block of 128 elements ------------
 
 constexpr int kBlock = 128;

@@ -337,8 +337,10 @@ hoccl_status_t balance_loss(const void *const *logits, const void *const *choice
     TRY(call.open(stream));
     const int wg = call.budget(a.first[batches]);
     TRY(call.launch(wg, [&] { return launch_balance(a, o.logits_dtype, wg, stream); }));
-    const int fwg = call.budget((unsigned long long)batches);
-    TRY(call.launch(fwg, [&] { return launch_balance_finish(a, fwg, stream); }));
+    if (!balance_is_one(a)) {
+        const int fwg = call.budget((unsigned long long)batches);
+        TRY(call.launch(fwg, [&] { return launch_balance_finish(a, fwg, stream); }));
+    }
     call.done(bytes + nb * 4 * (size_t)(1 + 2 * o.experts + o.ranks));
     return HOCCL_OK;
 }
