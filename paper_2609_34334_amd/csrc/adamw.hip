@@ -21,6 +21,7 @@
 // Bound by memory: 28 bytes an element (fp32 parameters and states, bf16
 // gradients and copies), 16.1 with 8-bit states.
 #include <algorithm>
+#include <type_traits>
 
 #include "lanes.h"
 #include "shard_ops.h"
@@ -59,11 +60,28 @@ __device__ __forceinline__ float step_one(const Hyper &h, float p, float g, floa
     return p * h.decay - h.rate * m * __builtin_amdgcn_rcpf(r * h.root + h.eps);
 }
 
+template <class T, bool NT, bool FULL, int B>
+__device__ __forceinline__ void load(const void *p, uint64_t e, uint64_t n, Raw<B> &r) {
+    if constexpr (FULL) load_raw<NT>(r, (const char *)p + e * T::size);
+    else load_window<T, NT>(p, e, n, r);
+}
+template <class T, bool FULL>
+__device__ __forceinline__ void store(void *p, uint64_t e, uint64_t n, const float (&f)[kVE]) {
+    if constexpr (FULL) {
+        Raw<T::size * kVE> r;
+        T::template pack<kVE>(f, r);
+        store_raw<kNT>((char *)p + e * T::size, r);
+    } else {
+        store_some<T, kNT>(p, e, n, f);
+    }
+}
+
 // The two vectors' moments as e4m3 bytes and scales.  The four blocks that 32
 // lanes hold (m and the root of v, twice) share the divisions for their
 // scales: every lane of a quad makes those of one block and gives the result
 // to the other three.
-__device__ __forceinline__ void put_blocks(const AdamSeg &s, uint64_t base, const float (&m)[2][kVE],
+template <bool FULL>
+__device__ __forceinline__ void put_blocks(const AdamSeg &s, uint64_t base, uint64_t n, const float (&m)[2][kVE],
                                            const float (&r)[2][kVE]) {
     constexpr int L = kBlock / kVE;
     const uint32_t q = threadIdx.x % 4;
@@ -90,39 +108,64 @@ __device__ __forceinline__ void put_blocks(const AdamSeg &s, uint64_t base, cons
         Raw<kVE> a, b;
         to_e4m3(x, a);
         to_e4m3(y, b);
-        store_bytes(s.m, e, s.n, a);
-        store_bytes(s.v, e, s.n, b);
+        if constexpr (FULL) {
+            store_raw((char *)s.m + e, a);
+            store_raw((char *)s.v + e, b);
+        } else {
+            store_bytes(s.m, e, n, a);
+            store_bytes(s.v, e, n, b);
+        }
     }
     const uint64_t first = base + (uint64_t)(q / 2 * kOpThreads + threadIdx.x / L * L) * kVE;
-    if (threadIdx.x % L < 4 && first < s.n) (q % 2 ? s.v_scale : s.m_scale)[first / kBlock] = scale;
+    if (threadIdx.x % L < 4 && (FULL || first < n)) (q % 2 ? s.v_scale : s.m_scale)[first / kBlock] = scale;
 }
 
-template <class TP, class TG, bool Q8>
+// FULL: the tile ends before the tensor does.
+template <class TP, class TG, bool Q8, bool FULL>
 __device__ __forceinline__ void tile(const AdamSeg &s, const Hyper &h, uint64_t base) {
     constexpr int U = kU<Q8>;
-    const uint64_t n = s.n;
+    const uint64_t n = FULL ? base + kTile<Q8> : s.n;
     float p[U][kVE], g[U][kVE], m[U][kVE], v[U][kVE];
+    using TS = std::conditional_t<Q8, EByte, EF32>;
+    Raw<TP::size * kVE> rp[U];
+    Raw<TG::size * kVE> rg[U];
+    Raw<TS::size * kVE> rm[U], rv[U];
+    float sm[U], sv[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         const uint64_t e = base + (uint64_t)(u * kOpThreads + threadIdx.x) * kVE;
-        load_some<TP, kNT>(s.param, e, n, p[u]);
-        load_some<TG, kNT>(s.grad, e, n, g[u]);
+        load<TP, kNT, FULL>(s.param, e, n, rp[u]);
+        load<TG, kNT, FULL>(s.grad, e, n, rg[u]);
+        load<TS, kNT && !Q8, FULL>(s.m, e, n, rm[u]);
+        load<TS, kNT && !Q8, FULL>(s.v, e, n, rv[u]);
         if constexpr (Q8) {
-            Raw<kVE> a, b;
-            load_bytes(s.m, e, n, a);
-            load_bytes(s.v, e, n, b);
-            const float sm = e < n ? s.m_scale[e / kBlock] : 0.0f, sv = e < n ? s.v_scale[e / kBlock] : 0.0f;
-            from_e4m3(a, m[u]);
-            from_e4m3(b, v[u]);
+            const uint64_t block = (FULL || e < n ? e : n - 1) / kBlock;
+            sm[u] = s.m_scale[block], sv[u] = s.v_scale[block];
+        }
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        const uint64_t e = base + (uint64_t)(u * kOpThreads + threadIdx.x) * kVE;
+        if constexpr (!FULL) {
+            settle_window<TP>(e, n, rp[u]);
+            settle_window<TG>(e, n, rg[u]);
+            settle_window<TS>(e, n, rm[u]);
+            settle_window<TS>(e, n, rv[u]);
+        }
+        TP::template unpack<kVE>(rp[u], p[u]);
+        TG::template unpack<kVE>(rg[u], g[u]);
+        if constexpr (Q8) {
+            from_e4m3(rm[u], m[u]);
+            from_e4m3(rv[u], v[u]);
 #pragma unroll
             for (int i = 0; i < kVE; ++i) {
-                m[u][i] *= sm;
-                const float r = v[u][i] * sv;
+                m[u][i] *= sm[u];
+                const float r = v[u][i] * sv[u];
                 v[u][i] = r * r;
             }
         } else {
-            load_some<EF32, kNT>(s.m, e, n, m[u]);
-            load_some<EF32, kNT>(s.v, e, n, v[u]);
+            EF32::unpack<kVE>(rm[u], m[u]);
+            EF32::unpack<kVE>(rv[u], v[u]);
         }
     }
     float r[U][kVE];
@@ -132,14 +175,14 @@ __device__ __forceinline__ void tile(const AdamSeg &s, const Hyper &h, uint64_t 
 #pragma unroll
         for (int i = 0; i < kVE; ++i) p[u][i] = step_one(h, p[u][i], g[u][i], m[u][i], v[u][i], r[u][i]);
         if constexpr (!Q8) {
-            store_some<EF32, kNT>(s.m, e, n, m[u]);
-            store_some<EF32, kNT>(s.v, e, n, v[u]);
+            store<EF32, FULL>(s.m, e, n, m[u]);
+            store<EF32, FULL>(s.v, e, n, v[u]);
         }
-        store_some<TP, kNT>(s.param, e, n, p[u]);
-        if (s.copy) store_some<EBF16, kNT>(s.copy, e, n, p[u]);
+        store<TP, FULL>(s.param, e, n, p[u]);
+        if (s.copy) store<EBF16, FULL>(s.copy, e, n, p[u]);
     }
     // Behind the end m and v are zero: nothing there is the largest of a block.
-    if constexpr (Q8) put_blocks(s, base, m, r);
+    if constexpr (Q8) put_blocks<FULL>(s, base, n, m, r);
 }
 
 template <class TP, class TG, bool Q8, int CAP>
@@ -162,7 +205,10 @@ __global__ void __launch_bounds__(kOpThreads) adamw_kernel(AdamArgsT<CAP>) {
         // would wait for six.
         const uint32_t i = threadIdx.x % 64;
         const int seg = __popcll(__ballot(i < (uint32_t)a.nseg && a.first[i < CAP ? i : 0] <= t)) - 1;
-        tile<TP, TG, Q8>(a.seg[seg], h, (uint64_t)(t - a.first[seg]) * kTile<Q8>);
+        const AdamSeg &s = a.seg[seg];
+        const uint64_t base = (uint64_t)(t - a.first[seg]) * kTile<Q8>;
+        if (s.n - base >= kTile<Q8>) tile<TP, TG, Q8, true>(s, h, base);
+        else tile<TP, TG, Q8, false>(s, h, base);
     }
 }
 

@@ -91,16 +91,18 @@ struct Logits {
     // As they are read, and as numbers.
     struct Packed {
         Raw<16> v[NV];
-        // `E`: 0 reads nothing.
         __device__ __forceinline__ void load(const void *p, int lane, int E) {
 #pragma unroll
-            for (int j = 0; j < NV; ++j) load_vector<T>(p, at(j, lane), E, v[j]);
+            for (int j = 0; j < NV; ++j) load_window<T>(p, at(j, lane), E, v[j]);
         }
     };
     float v[NV][VE];
-    __device__ __forceinline__ explicit Logits(const Packed &x) {
+    __device__ __forceinline__ Logits(Packed x, int lane, int E) {
 #pragma unroll
-        for (int j = 0; j < NV; ++j) T::template unpack<VE>(x.v[j], v[j]);
+        for (int j = 0; j < NV; ++j) {
+            if (E < L * N) settle_window<T>(at(j, lane), E, x.v[j]);
+            T::template unpack<VE>(x.v[j], v[j]);
+        }
     }
     static __device__ __forceinline__ int at(int j, int lane) { return (j * L + lane) * VE; }
     __device__ __forceinline__ void store(void *p, int lane, int E) const {
@@ -245,13 +247,14 @@ __global__ void __launch_bounds__(kThreads) balance_kernel(BalanceArgs) {
         auto load = [&](uint64_t row0) {
             const char *logits = (const char *)s.logits + row0 * E * T::size;
             const char *experts = (const char *)s.experts + row0 * k * (a.index64 ? 8 : 4);
-            const uint64_t left = row0 < s.tokens ? s.tokens - row0 : 0;
+            const uint64_t left = s.tokens - row0;
 #pragma unroll
             for (int u = 0; u < kAhead; ++u) {
-                // A row behind the last reads nothing and is padding.
+                // A row behind the last reads the pass's first instead and,
+                // without choices, is padding.
                 const uint32_t row = u * ROWS + slot;
                 const bool in = row < left;
-                next[u].load(logits + row * (uint32_t)E * T::size, lane, in ? E : 0);
+                next[u].load(logits + (in ? row : 0) * (uint32_t)E * T::size, lane, E);
                 next_first[u] = in && lane < k ? choice(a, experts, row * k + lane) : -1;
             }
         };
@@ -288,7 +291,7 @@ __global__ void __launch_bounds__(kThreads) balance_kernel(BalanceArgs) {
                     const int d = i * L + lane;
                     sent[i] += ((d < 32 ? lo : hi) >> (d & 31)) & 1u;
                 }
-                X x(now[u]);
+                X x(now[u], lane, E);
                 const float inv = x.softmax(lane, E);
 #pragma unroll
                 for (int j = 0; j < X::NV; ++j)
@@ -411,7 +414,7 @@ __global__ void __launch_bounds__(kOpThreads) balance_backward_kernel(BalanceArg
             for (int u = 0; u < kAhead; ++u) {
                 const uint32_t row = u * ROWS + slot;
                 const bool in = row < left;
-                now[u].load(logits + row * (uint32_t)E * T::size, lane, in ? E : 0);
+                now[u].load(logits + (in ? row : 0) * (uint32_t)E * T::size, lane, E);
                 any[u] = in && lane < k && choice(a, experts, row * k + lane) >= 0;
             }
 #pragma unroll
@@ -419,7 +422,7 @@ __global__ void __launch_bounds__(kOpThreads) balance_backward_kernel(BalanceArg
                 const uint32_t row = u * ROWS + slot;
                 const bool in = row < left;
                 more_choices<L>(a, experts, row * k, lane, in ? k : 0, [&](int e) { any[u] |= e >= 0; });
-                X x(now[u]);
+                X x(now[u], lane, E);
                 if (any_lane<L>(any[u])) {
                     const float inv = x.softmax(lane, E), scale = g * inv;
                     float dot = 0.0f;

@@ -113,39 +113,61 @@ __device__ __forceinline__ V here(V v) {
     return v;
 }
 
-// A vector of 16 bytes of `p` from element e on; elements at and behind `end`
-// are zeros and are not read.
-template <class T, bool NT = false, typename I>
-__device__ __forceinline__ void load_vector(const void *p, I e, I end, Raw<16> &r) {
-    constexpr int N = 16 / T::size;
-    if (e + N <= end) {
-        load_raw<NT>(r, (const char *)p + (size_t)e * T::size);
+// r shifted down by `bytes` (0 to B), zeros from above.
+template <int B>
+__device__ __forceinline__ void shift_down(Raw<B> &r, uint32_t bytes) {
+    constexpr int W = B / 4;
+#pragma unroll
+    for (int s = W; s >= 1; s /= 2)
+        if (bytes & (4 * s))
+#pragma unroll
+            for (int i = 0; i < W; ++i) r.w[i] = i + s < W ? r.w[i + s] : 0;
+#pragma unroll
+    for (int i = 0; i < W; ++i)
+        r.w[i] = __builtin_amdgcn_alignbit(i + 1 < W ? r.w[i + 1] : 0, r.w[i], bytes % 4 * 8);
+}
+
+// N elements of `p` from element e on, in two steps.  load_window reads them
+// or, where fewer than N are left before `end`, the N that end there, so that
+// every lane makes the same one read; settle_window moves what was read to
+// its place and makes zeros of elements at and behind `end`.  (Read element by
+// element, the ends of rows of 5003 bf16 waited for memory eight times: the
+// gradients of 6706 such rows took 129 us.)  Only where there are fewer than N
+// elements in all are they read one by one.  Any e is allowed.
+template <class T, bool NT = false, int B, typename I>
+__device__ __forceinline__ void load_window(const void *p, I e, I end, Raw<B> &r) {
+    constexpr I N = B / T::size;
+    if (end >= N) {
+        load_raw<NT>(r, (const char *)p + (size_t)(e + N <= end ? e : end - N) * T::size);
     } else {
         e = here(e);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) r.w[i] = 0;
+        for (int i = 0; i < B / 4; ++i) r.w[i] = 0;
 #pragma unroll
-        for (int i = 0; i < N; ++i)
+        for (int i = 0; i < (int)N; ++i)
             if (e + i < end) {
                 if constexpr (T::size == 4) r.w[i] = ((const uint32_t *)p)[e + i];
-                else r.w[i / 2] |= (uint32_t)((const uint16_t *)p)[e + i] << (16 * (i % 2));
+                else if constexpr (T::size == 2) r.w[i / 2] |= (uint32_t)((const uint16_t *)p)[e + i] << (16 * (i % 2));
+                else r.w[i / 4] |= (uint32_t)((const uint8_t *)p)[e + i] << (8 * (i % 4));
             }
     }
 }
+template <class T, int B, typename I>
+__device__ __forceinline__ void settle_window(I e, I end, Raw<B> &r) {
+    constexpr I N = B / T::size;
+    if (end >= N && e + N > end) {
+        const I s = e + N - end;
+        shift_down(r, (uint32_t)(s < N ? s : N) * T::size);
+    }
+}
 
-// N elements of `p` from element e on; those at and behind `end` are zeros
-// and are not read.
+// Both steps: N elements, as numbers.
 template <class T, bool NT = false, int N, typename I>
 __device__ __forceinline__ void load_some(const void *p, I e, I end, float (&f)[N]) {
-    if (e + N <= end) {
-        Raw<T::size * N> r;
-        load_raw<NT>(r, (const char *)p + (size_t)e * T::size);
-        T::template unpack<N>(r, f);
-    } else {
-        e = here(e);
-#pragma unroll
-        for (int i = 0; i < N; ++i) f[i] = e + i < end ? T::widen(((const typename T::S *)p)[e + i]) : 0.0f;
-    }
+    Raw<T::size * N> r;
+    load_window<T, NT>(p, e, end, r);
+    settle_window<T>(e, end, r);
+    T::template unpack<N>(r, f);
 }
 // Writes those of the N elements that lie before `end`.
 template <class T, bool NT = false, int N, typename I>
@@ -277,6 +299,10 @@ __device__ __forceinline__ uint32_t top_bits(const float (&f)[N]) {
     return t;
 }
 
+struct EByte {  // windows of e4m3 bytes
+    static constexpr int size = 1;
+};
+
 // N (4 or 8) floats of magnitude up to 448 to e4m3 bytes (round to nearest
 // even) and back.
 template <int N>
@@ -294,19 +320,6 @@ __device__ __forceinline__ void from_e4m3(const Raw<N> &r, float (&f)[N]) {
         const auto a = __builtin_amdgcn_cvt_pk_f32_fp8((int)r.w[i], false);
         const auto b = __builtin_amdgcn_cvt_pk_f32_fp8((int)r.w[i], true);
         f[4 * i] = a[0], f[4 * i + 1] = a[1], f[4 * i + 2] = b[0], f[4 * i + 3] = b[1];
-    }
-}
-template <bool NT = false, int N, typename I>
-__device__ __forceinline__ void load_bytes(const void *p, I e, I end, Raw<N> &r) {
-    if (e + N <= end) {
-        load_raw<NT>(r, (const char *)p + e);
-    } else {
-        e = here(e);
-#pragma unroll
-        for (int i = 0; i < N / 4; ++i) r.w[i] = 0;
-#pragma unroll
-        for (int i = 0; i < N; ++i)
-            if (e + i < end) r.w[i / 4] |= (uint32_t)((const uint8_t *)p)[e + i] << (8 * (i % 4));
     }
 }
 template <bool NT = false, int N, typename I>

@@ -51,21 +51,30 @@ __device__ __forceinline__ void load_weights(const void *w, int bf16, uint32_t e
     else load_some<EF32>(w, e, H, f);
 }
 
-// What a thread holds of a row: NV vectors.  WAVE: a wave a row, four rows a
-// workgroup; else a workgroup a row.
+// What a thread holds of a row: NV vectors.
 template <class T, int NV>
 struct Shaped {
     static constexpr int VE = kVE<T>, N = NV * VE;
     // Longer rows (over 8192 bf16 elements) have no registers for the next
-    // one, the longest none for the weights either, which they read again.
-    static constexpr bool ahead = N <= 8, keep_weights = N <= 16;
+    // one; the longest none for the weights, which they read again, nor, in the
+    // backward pass, for the residual's gradient, which is read last, and the
+    // weights' gradients, which stay in LDS (1677 rows of 20000 bf16: 141 us
+    // instead of 240; but 4092 rows of 8200 97 instead of 70).
+    static constexpr bool ahead = N <= 8, lean = NV >= 4, keep_weights = N <= 16;
     Raw<16> v[NV];
     // W threads a row, of which this is number t.
     template <bool NT>
     __device__ __forceinline__ void load(const void *p, uint64_t row, uint32_t H, uint32_t W, uint32_t t) {
         const char *at = (const char *)p + row * H * T::size;
 #pragma unroll
-        for (int j = 0; j < NV; ++j) load_vector<T, NT>(at, (j * W + t) * VE, H, v[j]);
+        for (int j = 0; j < NV; ++j) load_window<T, NT>(at, (j * W + t) * VE, H, v[j]);
+    }
+    __device__ __forceinline__ void settle(uint32_t H, uint32_t W, uint32_t t) {
+        uint32_t whole = W * N;
+        asm volatile("" : "+s"(whole));  // else the callers' loops are made twice
+        if (H == whole) return;          // no vector ends early
+#pragma unroll
+        for (int j = 0; j < NV; ++j) settle_window<T>((j * W + t) * VE, H, v[j]);
     }
     __device__ __forceinline__ void unpack(int j, float (&f)[VE]) const { T::template unpack<VE>(v[j], f); }
     // The same values, which the compiler takes for others: what it unpacked
@@ -81,11 +90,11 @@ struct Shaped {
 
 // M sums over a row's threads, the results in all of them.  `red` holds two
 // sets of the waves' sums, used in turn, so that one barrier is enough.
-template <bool WAVE, int M>
+template <int G, int M>
 __device__ __forceinline__ void row_sums(float (&v)[M], float (*red)[16][M], uint32_t waves, int &turn) {
 #pragma unroll
-    for (int m = 0; m < M; ++m) v[m] = join_lanes<64, LaneSum>(v[m]);
-    if constexpr (!WAVE) {
+    for (int m = 0; m < M; ++m) v[m] = join_lanes<G ? G : 64, LaneSum>(v[m]);
+    if constexpr (G == 0) {
         float(*mine)[M] = red[turn];
         turn ^= 1;
         if (threadIdx.x % 64 == 0)
@@ -98,16 +107,17 @@ __device__ __forceinline__ void row_sums(float (&v)[M], float (*red)[16][M], uin
     }
 }
 
-template <class T, bool WAVE, int NV, bool Q8>
-__global__ void __launch_bounds__(WAVE ? kOpThreads : 1024) rmsnorm_kernel(const RmsArgs a) {
+// G: lanes of a row, 256 / G rows a workgroup; 0: a workgroup a row.
+template <class T, int G, int NV, bool Q8>
+__global__ void __launch_bounds__(G ? kOpThreads : 1024) rmsnorm_kernel(const RmsArgs a) {
     using X = Shaped<T, NV>;
-    constexpr int VE = X::VE, ROWS = WAVE ? kOpThreads / 64 : 1;
+    constexpr int VE = X::VE, ROWS = G ? kOpThreads / G : 1;
     __shared__ float red[2][16][1];
     int turn = 0;
-    const uint32_t H = a.hidden, W = WAVE ? 64 : a.threads, t = WAVE ? threadIdx.x % 64 : threadIdx.x;
+    const uint32_t H = a.hidden, W = G ? G : a.threads, t = G ? threadIdx.x % G : threadIdx.x;
     const uint32_t nblk = (H + kBlock - 1) / kBlock;
     const uint64_t step = (uint64_t)gridDim.x * ROWS;
-    uint64_t row = (uint64_t)blockIdx.x * ROWS + (WAVE ? threadIdx.x / 64 : 0);
+    uint64_t row = (uint64_t)blockIdx.x * ROWS + (G ? threadIdx.x / G : 0);
     X x, res;
     auto load = [&](uint64_t r) {
         x.template load<false>(a.x, r, H, W, t);
@@ -122,6 +132,8 @@ __global__ void __launch_bounds__(WAVE ? kOpThreads : 1024) rmsnorm_kernel(const
         const uint64_t at = row * H * T::size;
         float h[NV][VE], sum[1] = {0.0f};
         if (!X::ahead) load(row);
+        x.settle(H, W, t);
+        if (a.residual) res.settle(H, W, t);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             x.unpack(j, h[j]);
@@ -139,7 +151,7 @@ __global__ void __launch_bounds__(WAVE ? kOpThreads : 1024) rmsnorm_kernel(const
 #pragma unroll
             for (int i = 0; i < VE; ++i) sum[0] += h[j][i] * h[j][i];
         }
-        row_sums<WAVE>(sum, red, W / 64, turn);
+        row_sums<G>(sum, red, W / 64, turn);
         const float r = 1.0f / __builtin_sqrtf(sum[0] / (float)H + a.eps);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
@@ -152,7 +164,7 @@ __global__ void __launch_bounds__(WAVE ? kOpThreads : 1024) rmsnorm_kernel(const
                 // Zeros behind the end, where 0 / 0 may have left a NaN.
 #pragma unroll
                 for (int i = 0; i < VE; ++i) y[i] = e + i < H ? y[i] : 0.0f;
-                const float top = __uint_as_float(join_lanes<kBlock / VE, LaneUMax>(top_bits(y)));
+                const float top = __uint_as_float(join_lanes<(G && G < kBlock / VE ? G : kBlock / VE), LaneUMax>(top_bits(y)));
                 float scale, inverse;
                 block_scale(top, scale, inverse);
 #pragma unroll
@@ -171,21 +183,22 @@ __global__ void __launch_bounds__(WAVE ? kOpThreads : 1024) rmsnorm_kernel(const
 // Backward.  Every thread keeps the sums of its columns' weight gradients in
 // registers over the rows of a partial sum; the rows of one partial are
 // those `blocks` apart.
-template <class T, bool WAVE, int NV>
-__global__ void __launch_bounds__(WAVE ? kOpThreads : 1024) rmsnorm_backward_kernel(const RmsBackArgs a) {
+template <class T, int G, int NV>
+__global__ void __launch_bounds__(G ? kOpThreads : 1024) rmsnorm_backward_kernel(const RmsBackArgs a) {
     using X = Shaped<T, NV>;
-    constexpr int VE = X::VE, ROWS = WAVE ? kOpThreads / 64 : 1;
+    constexpr int VE = X::VE, ROWS = G ? kOpThreads / G : 1;
     __shared__ float red[2][16][2];
-    __shared__ float cols[WAVE ? 64 * VE : 1];
+    __shared__ float cols[G ? G * VE : 1];
+    extern __shared__ float4 grads[];  // lean: a row's, each thread its own
     int turn = 0;
-    const uint32_t H = a.hidden, W = WAVE ? 64 : a.threads, t = WAVE ? threadIdx.x % 64 : threadIdx.x;
-    const int slot = WAVE ? threadIdx.x / 64 : 0;
+    const uint32_t H = a.hidden, W = G ? G : a.threads, t = G ? threadIdx.x % G : threadIdx.x;
+    const int slot = G ? threadIdx.x / G : 0;
     const uint64_t step = (uint64_t)a.blocks * ROWS;
     X h, g, d;
     auto load = [&](uint64_t r) {
         h.template load<true>(a.h, r, H, W, t);
         g.template load<true>(a.dy, r, H, W, t);
-        if (a.dres) d.template load<true>(a.dres, r, H, W, t);
+        if (!X::lean && a.dres) d.template load<true>(a.dres, r, H, W, t);
     };
     float w[NV][VE];
     if (X::keep_weights)
@@ -193,12 +206,18 @@ __global__ void __launch_bounds__(WAVE ? kOpThreads : 1024) rmsnorm_backward_ker
         for (int j = 0; j < NV; ++j) load_weights(a.weight, a.weight_bf16, (j * W + t) * VE, H, w[j]);
     for (uint32_t part = blockIdx.x; part < a.blocks; part += gridDim.x) {
         float dw[NV][VE] = {};
+        if constexpr (X::lean)
+#pragma unroll
+            for (int j = 0; j < X::N / 4; ++j) grads[j * W + t] = make_float4(0, 0, 0, 0);
         uint64_t row = (uint64_t)part * ROWS + slot;
         if (X::ahead && row < a.rows) load(row);
         for (; row < a.rows; row += step) {
             if (!X::ahead) load(row);
             X now_h = h, now_g = g, now_d = d;
             if (X::ahead && row + step < a.rows) load(row + step);
+            now_h.settle(H, W, t);
+            now_g.settle(H, W, t);
+            if (!X::lean && a.dres) now_d.settle(H, W, t);
             float sums[2] = {0.0f, 0.0f};
 #pragma unroll
             for (int j = 0; j < NV; ++j) {
@@ -212,7 +231,7 @@ __global__ void __launch_bounds__(WAVE ? kOpThreads : 1024) rmsnorm_backward_ker
                     sums[1] += y[i] * w[j][i] * u[i];
                 }
             }
-            row_sums<WAVE>(sums, red, W / 64, turn);
+            row_sums<G>(sums, red, W / 64, turn);
             const float r = 1.0f / __builtin_sqrtf(sums[0] / (float)H + a.eps);
             const float c = sums[1] / (float)H * r * r;
             now_h.forget(), now_g.forget();
@@ -221,34 +240,60 @@ __global__ void __launch_bounds__(WAVE ? kOpThreads : 1024) rmsnorm_backward_ker
                 float u[VE], y[VE], x[VE] = {};
                 now_h.unpack(j, u);
                 now_g.unpack(j, y);
-                if (a.dres) now_d.unpack(j, x);
+                if (X::lean && a.dres)
+                    load_some<T, true>((const char *)a.dres + row * H * T::size, (j * W + t) * VE, H, x);
+                else if (a.dres)
+                    now_d.unpack(j, x);
                 if (!X::keep_weights) load_weights(a.weight, a.weight_bf16, (j * W + t) * VE, H, w[j]);
 #pragma unroll
-                for (int i = 0; i < VE; ++i) {
-                    x[i] += r * (y[i] * w[j][i] - u[i] * c);
-                    dw[j][i] += y[i] * (u[i] * r);
+                for (int i = 0; i < VE; ++i) x[i] += r * (y[i] * w[j][i] - u[i] * c);
+                if constexpr (X::lean) {
+#pragma unroll
+                    for (int i = 0; i < VE; i += 4) {
+                        float4 &q = grads[(j * VE + i) / 4 * W + t];
+                        float4 v = q;
+                        v.x += y[i] * (u[i] * r), v.y += y[i + 1] * (u[i + 1] * r);
+                        v.z += y[i + 2] * (u[i + 2] * r), v.w += y[i + 3] * (u[i + 3] * r);
+                        q = v;
+                    }
+                } else {
+#pragma unroll
+                    for (int i = 0; i < VE; ++i) dw[j][i] += y[i] * (u[i] * r);
                 }
                 store_some<T, true>((char *)a.dx + row * H * T::size, (j * W + t) * VE, H, x);
             }
         }
         if (!a.partial) continue;
         float *out = a.partial + (uint64_t)part * H;
-        if constexpr (WAVE) {
-            // The workgroup's rows in turn, so that the order is fixed.
-            for (int s = 0; s < ROWS; ++s) {
-                if (slot == s)
+        if constexpr (G > 0) {
+            // A wave's rows, then the waves in turn, so that the order is
+            // fixed.
+            constexpr int WAVES = kOpThreads / 64;
+            const int wave = threadIdx.x / 64;
+#pragma unroll
+            for (int i = 0; i < VE; ++i) dw[0][i] = join_groups<G, LaneSum>(dw[0][i]);
+            for (int s = 0; s < WAVES; ++s) {
+                if (wave == s && threadIdx.x % 64 < G)
 #pragma unroll
                     for (int i = 0; i < VE; ++i) {
-                        float &c = cols[i * 64 + t];
+                        float &c = cols[i * G + t];
                         c = s ? c + dw[0][i] : dw[0][i];
-                        if (s == ROWS - 1) dw[0][i] = c;
+                        if (s == WAVES - 1) dw[0][i] = c;
                     }
                 __syncthreads();
             }
-            if (slot != ROWS - 1) continue;
+            if (wave != WAVES - 1 || threadIdx.x % 64 >= G) continue;
         }
 #pragma unroll
-        for (int j = 0; j < NV; ++j) store_some<EF32>(out, (j * W + t) * VE, H, dw[j]);
+        for (int j = 0; j < NV; ++j) {
+            if constexpr (X::lean)
+#pragma unroll
+                for (int i = 0; i < VE; i += 4) {
+                    const float4 v = grads[(j * VE + i) / 4 * W + t];
+                    dw[j][i] = v.x, dw[j][i + 1] = v.y, dw[j][i + 2] = v.z, dw[j][i + 3] = v.w;
+                }
+            store_some<EF32>(out, (j * W + t) * VE, H, dw[j]);
+        }
     }
 }
 
@@ -275,33 +320,40 @@ __global__ void __launch_bounds__(1024) weight_grad_kernel(const float *partial,
     }
 }
 
-// Threads of a row and vectors of a thread: as few threads as hold the row,
-// whole waves.
+// Threads of a row and vectors of a thread: 8 to 64 lanes of a wave or as few
+// waves as hold the row.
 struct Shape {
     int W, NV;
 };
 Shape shape_of(size_t hidden, hoccl_dtype_t dt) {
     const size_t per = dt == HOCCL_BF16 ? kVE<EBF16> : kVE<EF32>, v = (hidden + per - 1) / per;
+    if (v <= 64) return {v <= 8 ? 8 : v <= 16 ? 16 : v <= 32 ? 32 : 64, 1};
     int n = 1;
     while (v > (size_t)(1024 * n)) n *= 2;
     return {(int)((v + 64 * n - 1) / (64 * n)) * 64, n};
 }
-int group_of(int W) { return W == 64 ? kOpThreads : W; }  // threads of a workgroup
-int rows_of(int W) { return group_of(W) / W; }
+int group_of(Shape s) { return s.W <= 64 ? kOpThreads : s.W; }  // threads of a workgroup
+int rows_of(Shape s) { return group_of(s) / s.W; }
 
-// f(T, WAVE, NV) of a row's element type and shape.
+// f(T, G, NV) of a row's element type and shape.
 template <class F>
 const void *with_shape(hoccl_dtype_t dt, Shape s, F &&f) {
-    auto typed = [&](auto wave, auto n) { return dt == HOCCL_BF16 ? f(EBF16(), wave, n) : f(EF32(), wave, n); };
-    using std::integral_constant;
-    if (s.W == 64) return typed(std::true_type(), integral_constant<int, 1>());
-    switch (s.NV) {
-    case 1: return typed(std::false_type(), integral_constant<int, 1>());
-    case 2: return typed(std::false_type(), integral_constant<int, 2>());
-    case 4: return typed(std::false_type(), integral_constant<int, 4>());
+    auto typed = [&](auto g, auto n) { return dt == HOCCL_BF16 ? f(EBF16(), g, n) : f(EF32(), g, n); };
+#define HOCCL_SHAPE(g, n) typed(std::integral_constant<int, g>(), std::integral_constant<int, n>())
+    switch (s.W) {
+    case 8: return HOCCL_SHAPE(8, 1);
+    case 16: return HOCCL_SHAPE(16, 1);
+    case 32: return HOCCL_SHAPE(32, 1);
+    case 64: return HOCCL_SHAPE(64, 1);
     }
+    switch (s.NV) {
+    case 1: return HOCCL_SHAPE(0, 1);
+    case 2: return HOCCL_SHAPE(0, 2);
+    case 4: return HOCCL_SHAPE(0, 4);
+    }
+#undef HOCCL_SHAPE
     // fp32 alone: 32768 bf16 are four vectors a thread.
-    return f(EF32(), std::false_type(), integral_constant<int, 8>());
+    return f(EF32(), std::integral_constant<int, 0>(), std::integral_constant<int, 8>());
 }
 
 }  // namespace
@@ -310,45 +362,50 @@ const void *with_shape(hoccl_dtype_t dt, Shape s, F &&f) {
 // of them: 48.5 us instead of 44.9 at 8192 x 4096, 14.1 instead of 12.6 at 4096
 // x 2048 into 8 bits.
 constexpr unsigned kForwardThreads = 2048;
-// Threads of the backward pass, as many partial sums as that makes workgroups:
-// 1024 for each of 256 CUs.  Twice as many took 109 us instead of 104 at 16384
-// x 4096, half as many 121.
-constexpr size_t kBackwardThreads = 256 * 1024;
+// Workgroups of the backward pass, and partial sums: as many for each of 256
+// CUs as make about 1024 threads.  Twice as many took 109 us instead of 104 at
+// 16384 x 4096, half as many 121.
+size_t backward_groups(int threads) { return 256 * (size_t)std::max(1, (1024 + threads / 2) / threads); }
 
 unsigned long long rmsnorm_workgroups(size_t rows, size_t hidden, hoccl_dtype_t dt, int cus) {
     const Shape s = shape_of(hidden, dt);
-    const unsigned long long groups = (rows + rows_of(s.W) - 1) / rows_of(s.W);
-    return std::min(groups, (unsigned long long)kForwardThreads / group_of(s.W) * cus);
+    const unsigned long long groups = (rows + rows_of(s) - 1) / rows_of(s);
+    return std::min(groups, (unsigned long long)kForwardThreads / group_of(s) * cus);
 }
 
 hipError_t launch_rmsnorm(RmsArgs a, hoccl_dtype_t dt, int wg, hipStream_t s) {
     const Shape sh = shape_of(a.hidden, dt);
-    const void *k = with_shape(dt, sh, [&](auto type, auto w, auto n) -> const void * {
+    const void *k = with_shape(dt, sh, [&](auto type, auto g, auto n) -> const void * {
         using T = decltype(type);
-        constexpr bool WAVE = decltype(w)::value;
-        constexpr int NV = decltype(n)::value;
-        return a.scale ? (const void *)rmsnorm_kernel<T, WAVE, NV, true>
-                       : (const void *)rmsnorm_kernel<T, WAVE, NV, false>;
+        constexpr int G = decltype(g)::value, NV = decltype(n)::value;
+        return a.scale ? (const void *)rmsnorm_kernel<T, G, NV, true> : (const void *)rmsnorm_kernel<T, G, NV, false>;
     });
     a.threads = (uint32_t)sh.W;
     void *args[] = {(void *)&a};
-    return hipLaunchKernel(k, dim3((unsigned)wg), dim3(group_of(sh.W)), args, 0, s);
+    return hipLaunchKernel(k, dim3((unsigned)wg), dim3(group_of(sh)), args, 0, s);
 }
 
 uint32_t rmsnorm_backward_blocks(size_t rows, size_t hidden, hoccl_dtype_t dt) {
-    const int W = shape_of(hidden, dt).W;
-    const size_t groups = (rows + rows_of(W) - 1) / rows_of(W);
-    return (uint32_t)std::min(groups, kBackwardThreads / group_of(W));
+    const Shape s = shape_of(hidden, dt);
+    const size_t groups = (rows + rows_of(s) - 1) / rows_of(s);
+    return (uint32_t)std::min(groups, backward_groups(group_of(s)));
 }
 
 hipError_t launch_rmsnorm_backward(RmsBackArgs a, hoccl_dtype_t dt, int wg, hipStream_t s) {
     const Shape sh = shape_of(a.hidden, dt);
-    const void *k = with_shape(dt, sh, [&](auto type, auto w, auto n) -> const void * {
-        return (const void *)rmsnorm_backward_kernel<decltype(type), decltype(w)::value, decltype(n)::value>;
+    size_t lds = 0;
+    const void *k = with_shape(dt, sh, [&](auto type, auto g, auto n) -> const void * {
+        using X = Shaped<decltype(type), decltype(n)::value>;
+        if (X::lean) lds = (size_t)sh.W * X::N * 4;
+        return (const void *)rmsnorm_backward_kernel<decltype(type), decltype(g)::value, decltype(n)::value>;
     });
+    if (lds > (size_t)48 << 10) {  // up to 128 KiB of a CU's 160
+        const hipError_t e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);
+        if (e != hipSuccess) return e;
+    }
     a.threads = (uint32_t)sh.W;
     void *args[] = {(void *)&a};
-    return hipLaunchKernel(k, dim3((unsigned)wg), dim3(group_of(sh.W)), args, 0, s);
+    return hipLaunchKernel(k, dim3((unsigned)wg), dim3(group_of(sh)), args, lds, s);
 }
 
 uint32_t rmsnorm_grad_workgroups(size_t hidden) { return (uint32_t)((hidden + kGradCols - 1) / kGradCols); }
