@@ -132,19 +132,24 @@ __global__ void __launch_bounds__(G ? kOpThreads : 1024) rmsnorm_kernel(const Rm
         const uint64_t at = row * H * T::size;
         float h[NV][VE], sum[1] = {0.0f};
         if (!X::ahead) load(row);
-        x.settle(H, W, t);
-        if (a.residual) res.settle(H, W, t);
+        // The next row's reads go out before this one's are waited for, or,
+        // where y is not in 8 bits, after: 8192 x 4096 in 8 bits 38.5 us and
+        // 42.1, else 49.9 and 47.6.
+        X now = x, now_res = res;
+        if (Q8 && X::ahead && row + step < a.rows) load(row + step);
+        now.settle(H, W, t);
+        if (a.residual) now_res.settle(H, W, t);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            x.unpack(j, h[j]);
+            now.unpack(j, h[j]);
             if (a.residual) {
                 float r[VE];
-                res.unpack(j, r);
+                now_res.unpack(j, r);
 #pragma unroll
                 for (int i = 0; i < VE; ++i) h[j][i] = T::widen(T::narrow(h[j][i] + r[i]));
             }
         }
-        if (X::ahead && row + step < a.rows) load(row + step);
+        if (!Q8 && X::ahead && row + step < a.rows) load(row + step);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             if (a.residual_out) store_some<T, true>((char *)a.residual_out + at, (j * W + t) * VE, H, h[j]);
