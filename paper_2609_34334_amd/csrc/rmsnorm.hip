@@ -27,8 +27,10 @@
 //
 // The backward pass reads and writes past the caches (105 us otherwise, 94 so,
 // at 16384 x 4096); the forward pass writes past them (4096 x 2048 into 8 bits
-// 12.5 and 11.5 us, 8192 x 4096 50.8 and 50.0) but reads through them, as its
-// inputs have mostly just been made (read past them 12.8 and 48.5).
+// 12.5 and 11.5 us, 8192 x 4096 50.8 and 50.0).  It reads through them, as its
+// inputs have mostly just been made, but where the call moves more than the
+// 256 MB that the last of them holds: 8192 x 4096 takes 43 us instead of 50,
+// 4096 x 2048, 59 MB, would take 12.7 instead of 11.1.
 //
 // Bound by memory: 8 bytes an element (bf16 with a residual), 7 with y in 8
 // bits; backward 8 bytes and the partial sums of the weight's gradient.
@@ -51,8 +53,10 @@ __device__ __forceinline__ void load_weights(const void *w, int bf16, uint32_t e
     else load_some<EF32>(w, e, H, f);
 }
 
-// What a thread holds of a row: NV vectors.
-template <class T, int NV>
+// What a thread holds of a row: NV vectors.  FULL: the vectors of the row's
+// threads end where it does (checking for it in the loop, the gradients at
+// 16384 x 4096 took 101 us instead of 95).
+template <class T, int NV, bool FULL>
 struct Shaped {
     static constexpr int VE = kVE<T>, N = NV * VE;
     // Longer rows (over 8192 bf16 elements) have no registers for the next
@@ -67,16 +71,27 @@ struct Shaped {
     __device__ __forceinline__ void load(const void *p, uint64_t row, uint32_t H, uint32_t W, uint32_t t) {
         const char *at = (const char *)p + row * H * T::size;
 #pragma unroll
-        for (int j = 0; j < NV; ++j) load_window<T, NT>(at, (j * W + t) * VE, H, v[j]);
+        for (int j = 0; j < NV; ++j) {
+            const uint32_t e = (j * W + t) * VE;
+            if constexpr (FULL) load_raw<NT>(v[j], at + e * T::size);
+            else load_window<T, NT>(at, e, H, v[j]);
+        }
     }
     __device__ __forceinline__ void settle(uint32_t H, uint32_t W, uint32_t t) {
-        uint32_t whole = W * N;
-        asm volatile("" : "+s"(whole));  // else the callers' loops are made twice
-        if (H == whole) return;          // no vector ends early
+        if constexpr (!FULL)
 #pragma unroll
         for (int j = 0; j < NV; ++j) settle_window<T>((j * W + t) * VE, H, v[j]);
     }
     __device__ __forceinline__ void unpack(int j, float (&f)[VE]) const { T::template unpack<VE>(v[j], f); }
+    static __device__ __forceinline__ void store(void *p, uint32_t e, uint32_t H, const float (&f)[VE]) {
+        if constexpr (FULL) {
+            Raw<16> r;
+            T::template pack<VE>(f, r);
+            store_raw<true>((char *)p + e * T::size, r);
+        } else {
+            store_some<T, true>(p, e, H, f);
+        }
+    }
     // The same values, which the compiler takes for others: what it unpacked
     // before need not stay in registers.
     __device__ __forceinline__ void forget() {
@@ -108,9 +123,10 @@ __device__ __forceinline__ void row_sums(float (&v)[M], float (*red)[16][M], uin
 }
 
 // G: lanes of a row, 256 / G rows a workgroup; 0: a workgroup a row.
-template <class T, int G, int NV, bool Q8>
+// FAR: reads past the caches.
+template <class T, int G, int NV, bool FULL, bool Q8, bool FAR>
 __global__ void __launch_bounds__(G ? kOpThreads : 1024) rmsnorm_kernel(const RmsArgs a) {
-    using X = Shaped<T, NV>;
+    using X = Shaped<T, NV, FULL>;
     constexpr int VE = X::VE, ROWS = G ? kOpThreads / G : 1;
     __shared__ float red[2][16][1];
     int turn = 0;
@@ -120,8 +136,8 @@ __global__ void __launch_bounds__(G ? kOpThreads : 1024) rmsnorm_kernel(const Rm
     uint64_t row = (uint64_t)blockIdx.x * ROWS + (G ? threadIdx.x / G : 0);
     X x, res;
     auto load = [&](uint64_t r) {
-        x.template load<false>(a.x, r, H, W, t);
-        if (a.residual) res.template load<false>(a.residual, r, H, W, t);
+        x.template load<FAR>(a.x, r, H, W, t);
+        if (a.residual) res.template load<FAR>(a.residual, r, H, W, t);
     };
     if (X::ahead && row < a.rows) load(row);
     float w[NV][VE];
@@ -152,7 +168,7 @@ __global__ void __launch_bounds__(G ? kOpThreads : 1024) rmsnorm_kernel(const Rm
         if (!Q8 && X::ahead && row + step < a.rows) load(row + step);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
-            if (a.residual_out) store_some<T, true>((char *)a.residual_out + at, (j * W + t) * VE, H, h[j]);
+            if (a.residual_out) X::store((char *)a.residual_out + at, (j * W + t) * VE, H, h[j]);
 #pragma unroll
             for (int i = 0; i < VE; ++i) sum[0] += h[j][i] * h[j][i];
         }
@@ -179,7 +195,7 @@ __global__ void __launch_bounds__(G ? kOpThreads : 1024) rmsnorm_kernel(const Rm
                 store_bytes<true>((char *)a.y + row * H, e, H, q);
                 if (e % kBlock == 0 && e < H) a.scale[row * nblk + e / kBlock] = scale;
             } else {
-                store_some<T, true>((char *)a.y + at, e, H, y);
+                X::store((char *)a.y + at, e, H, y);
             }
         }
     }
@@ -188,9 +204,9 @@ __global__ void __launch_bounds__(G ? kOpThreads : 1024) rmsnorm_kernel(const Rm
 // Backward.  Every thread keeps the sums of its columns' weight gradients in
 // registers over the rows of a partial sum; the rows of one partial are
 // those `blocks` apart.
-template <class T, int G, int NV>
+template <class T, int G, int NV, bool FULL>
 __global__ void __launch_bounds__(G ? kOpThreads : 1024) rmsnorm_backward_kernel(const RmsBackArgs a) {
-    using X = Shaped<T, NV>;
+    using X = Shaped<T, NV, FULL>;
     constexpr int VE = X::VE, ROWS = G ? kOpThreads / G : 1;
     __shared__ float red[2][16][2];
     __shared__ float cols[G ? G * VE : 1];
@@ -265,7 +281,7 @@ __global__ void __launch_bounds__(G ? kOpThreads : 1024) rmsnorm_backward_kernel
 #pragma unroll
                     for (int i = 0; i < VE; ++i) dw[j][i] += y[i] * (u[i] * r);
                 }
-                store_some<T, true>((char *)a.dx + row * H * T::size, (j * W + t) * VE, H, x);
+                X::store((char *)a.dx + row * H * T::size, (j * W + t) * VE, H, x);
             }
         }
         if (!a.partial) continue;
@@ -329,21 +345,31 @@ __global__ void __launch_bounds__(1024) weight_grad_kernel(const float *partial,
 // waves as hold the row.
 struct Shape {
     int W, NV;
+    bool full;
 };
 Shape shape_of(size_t hidden, hoccl_dtype_t dt) {
     const size_t per = dt == HOCCL_BF16 ? kVE<EBF16> : kVE<EF32>, v = (hidden + per - 1) / per;
-    if (v <= 64) return {v <= 8 ? 8 : v <= 16 ? 16 : v <= 32 ? 32 : 64, 1};
-    int n = 1;
-    while (v > (size_t)(1024 * n)) n *= 2;
-    return {(int)((v + 64 * n - 1) / (64 * n)) * 64, n};
+    Shape s;
+    if (v <= 64) {
+        s = {v <= 8 ? 8 : v <= 16 ? 16 : v <= 32 ? 32 : 64, 1, false};
+    } else {
+        int n = 1;
+        while (v > (size_t)(1024 * n)) n *= 2;
+        s = {(int)((v + 64 * n - 1) / (64 * n)) * 64, n, false};
+    }
+    s.full = (size_t)s.W * s.NV * per == hidden;
+    return s;
 }
 int group_of(Shape s) { return s.W <= 64 ? kOpThreads : s.W; }  // threads of a workgroup
 int rows_of(Shape s) { return group_of(s) / s.W; }
 
-// f(T, G, NV) of a row's element type and shape.
+// f(T, G, NV, FULL) of a row's element type and shape.
 template <class F>
 const void *with_shape(hoccl_dtype_t dt, Shape s, F &&f) {
-    auto typed = [&](auto g, auto n) { return dt == HOCCL_BF16 ? f(EBF16(), g, n) : f(EF32(), g, n); };
+    auto typed = [&](auto g, auto n) {
+        if (s.full) return dt == HOCCL_BF16 ? f(EBF16(), g, n, std::true_type()) : f(EF32(), g, n, std::true_type());
+        return dt == HOCCL_BF16 ? f(EBF16(), g, n, std::false_type()) : f(EF32(), g, n, std::false_type());
+    };
 #define HOCCL_SHAPE(g, n) typed(std::integral_constant<int, g>(), std::integral_constant<int, n>())
     switch (s.W) {
     case 8: return HOCCL_SHAPE(8, 1);
@@ -358,19 +384,25 @@ const void *with_shape(hoccl_dtype_t dt, Shape s, F &&f) {
     }
 #undef HOCCL_SHAPE
     // fp32 alone: 32768 bf16 are four vectors a thread.
-    return f(EF32(), std::integral_constant<int, 0>(), std::integral_constant<int, 8>());
+    return f(EF32(), std::integral_constant<int, 0>(), std::integral_constant<int, 8>(), std::false_type());
 }
 
 }  // namespace
+
+constexpr unsigned long long kCacheBytes = 256ull << 20;
 
 // Threads of a CU's workgroups in the forward pass: what it holds.  A quarter
 // of them: 48.5 us instead of 44.9 at 8192 x 4096, 14.1 instead of 12.6 at 4096
 // x 2048 into 8 bits.
 constexpr unsigned kForwardThreads = 2048;
 // Workgroups of the backward pass, and partial sums: as many for each of 256
-// CUs as make about 1024 threads.  Twice as many took 109 us instead of 104 at
-// 16384 x 4096, half as many 121.
-size_t backward_groups(int threads) { return 256 * (size_t)std::max(1, (1024 + threads / 2) / threads); }
+// CUs as make about 512 threads.  16384 x 4096 takes 92 us so and 99 with 1024
+// threads; but rows whose last vectors are not whole leave lanes idle and wait
+// more (640 bf16: 2.65 TB/s with 512, 3.95 with 1024).
+size_t backward_groups(Shape s) {
+    const int most = s.full ? 512 : 1024, threads = group_of(s);
+    return 256 * (size_t)std::max(1, (most + threads / 2) / threads);
+}
 
 unsigned long long rmsnorm_workgroups(size_t rows, size_t hidden, hoccl_dtype_t dt, int cus) {
     const Shape s = shape_of(hidden, dt);
@@ -378,12 +410,18 @@ unsigned long long rmsnorm_workgroups(size_t rows, size_t hidden, hoccl_dtype_t 
     return std::min(groups, (unsigned long long)kForwardThreads / group_of(s) * cus);
 }
 
-hipError_t launch_rmsnorm(RmsArgs a, hoccl_dtype_t dt, int wg, hipStream_t s) {
+hipError_t launch_rmsnorm(RmsArgs a, hoccl_dtype_t dt, unsigned long long bytes, int wg, hipStream_t s) {
+    const bool far = bytes > kCacheBytes;
     const Shape sh = shape_of(a.hidden, dt);
-    const void *k = with_shape(dt, sh, [&](auto type, auto g, auto n) -> const void * {
+    const void *k = with_shape(dt, sh, [&](auto type, auto g, auto n, auto full) -> const void * {
         using T = decltype(type);
         constexpr int G = decltype(g)::value, NV = decltype(n)::value;
-        return a.scale ? (const void *)rmsnorm_kernel<T, G, NV, true> : (const void *)rmsnorm_kernel<T, G, NV, false>;
+        constexpr bool FULL = decltype(full)::value;
+        if (a.scale)
+            return far ? (const void *)rmsnorm_kernel<T, G, NV, FULL, true, true>
+                       : (const void *)rmsnorm_kernel<T, G, NV, FULL, true, false>;
+        return far ? (const void *)rmsnorm_kernel<T, G, NV, FULL, false, true>
+                   : (const void *)rmsnorm_kernel<T, G, NV, FULL, false, false>;
     });
     a.threads = (uint32_t)sh.W;
     void *args[] = {(void *)&a};
@@ -393,16 +431,19 @@ hipError_t launch_rmsnorm(RmsArgs a, hoccl_dtype_t dt, int wg, hipStream_t s) {
 uint32_t rmsnorm_backward_blocks(size_t rows, size_t hidden, hoccl_dtype_t dt) {
     const Shape s = shape_of(hidden, dt);
     const size_t groups = (rows + rows_of(s) - 1) / rows_of(s);
-    return (uint32_t)std::min(groups, backward_groups(group_of(s)));
+    return (uint32_t)std::min(groups, backward_groups(s));
 }
 
 hipError_t launch_rmsnorm_backward(RmsBackArgs a, hoccl_dtype_t dt, int wg, hipStream_t s) {
     const Shape sh = shape_of(a.hidden, dt);
     size_t lds = 0;
-    const void *k = with_shape(dt, sh, [&](auto type, auto g, auto n) -> const void * {
-        using X = Shaped<decltype(type), decltype(n)::value>;
+    const void *k = with_shape(dt, sh, [&](auto type, auto g, auto n, auto full) -> const void * {
+        using T = decltype(type);
+        constexpr int G = decltype(g)::value, NV = decltype(n)::value;
+        constexpr bool FULL = decltype(full)::value;
+        using X = Shaped<T, NV, FULL>;
         if (X::lean) lds = (size_t)sh.W * X::N * 4;
-        return (const void *)rmsnorm_backward_kernel<decltype(type), decltype(g)::value, decltype(n)::value>;
+        return (const void *)rmsnorm_backward_kernel<T, G, NV, FULL>;
     });
     if (lds > (size_t)48 << 10) {  // up to 128 KiB of a CU's 160
         const hipError_t e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, (int)lds);

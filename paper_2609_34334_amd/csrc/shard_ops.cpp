@@ -52,6 +52,7 @@ size_t size_of(hoccl_dtype_t dt) { return dt == HOCCL_BF16 ? 2 : 4; }
 // for the pairs that a call allows by not adding the second of them.
 class Operands {
 public:
+    Operands() { all_.reserve(16); }
     // `align`: the element size.
     hoccl_status_t add(const void *p, size_t bytes, size_t align, bool written, const char *name, long index = -1) {
         if (!p && bytes) return index < 0 ? invalid("%s is NULL", name) : invalid("%s[%ld] is NULL", name, index);
@@ -209,10 +210,11 @@ hoccl_status_t rmsnorm(const void *x, const void *residual, const void *weight, 
     OpCall call;
     TRY(call.open(stream));
     const RmsArgs a = {x, residual, weight, residual_out, y, scale, rows, (uint32_t)hidden, wdt == HOCCL_BF16, (float)eps, 0};
+    const unsigned long long moved = (unsigned long long)bytes * (1 + (residual != nullptr) + (residual_out != nullptr)) +
+                                     (scale ? rows * (hidden + blocks * 4) : bytes) + hidden * size_of(wdt);
     const int wg = call.budget(rmsnorm_workgroups(rows, hidden, dt, call.cus()));
-    TRY(call.launch(wg, [&] { return launch_rmsnorm(a, dt, wg, stream); }));
-    call.done((unsigned long long)bytes * (1 + (residual != nullptr) + (residual_out != nullptr)) +
-              (scale ? rows * (hidden + blocks * 4) : bytes) + hidden * size_of(wdt));
+    TRY(call.launch(wg, [&] { return launch_rmsnorm(a, dt, moved, wg, stream); }));
+    call.done(moved);
     return HOCCL_OK;
 }
 

@@ -76,7 +76,8 @@ struct RmsBackArgs {
 
 // Workgroups of the automatic launch.
 unsigned long long rmsnorm_workgroups(size_t rows, size_t hidden, hoccl_dtype_t dt, int cus);
-hipError_t launch_rmsnorm(RmsArgs a, hoccl_dtype_t dt, int wg, hipStream_t s);
+// `bytes`: what the call moves.
+hipError_t launch_rmsnorm(RmsArgs a, hoccl_dtype_t dt, unsigned long long bytes, int wg, hipStream_t s);
 // Partial sums of the weight's gradient: a number that goes by the sizes
 // alone, so that the result does not depend on the workgroups.
 uint32_t rmsnorm_backward_blocks(size_t rows, size_t hidden, hoccl_dtype_t dt);
