@@ -286,6 +286,7 @@ __global__ void __launch_bounds__(G ? kOpThreads : 1024) rmsnorm_backward_kernel
         }
         if (!a.partial) continue;
         float *out = a.partial + (uint64_t)part * H;
+        bool mine = true;  // the threads that hold the sums
         if constexpr (G > 0) {
             // A wave's rows, then the waves in turn, so that the order is
             // fixed.
@@ -303,7 +304,7 @@ __global__ void __launch_bounds__(G ? kOpThreads : 1024) rmsnorm_backward_kernel
                     }
                 __syncthreads();
             }
-            if (wave != WAVES - 1 || threadIdx.x % 64 >= G) continue;
+            mine = wave == WAVES - 1 && threadIdx.x % 64 < G;
         }
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
@@ -313,7 +314,7 @@ __global__ void __launch_bounds__(G ? kOpThreads : 1024) rmsnorm_backward_kernel
                     const float4 v = grads[(j * VE + i) / 4 * W + t];
                     dw[j][i] = v.x, dw[j][i + 1] = v.y, dw[j][i + 2] = v.z, dw[j][i + 3] = v.w;
                 }
-            store_some<EF32>(out, (j * W + t) * VE, H, dw[j]);
+            if (mine) store_some<EF32>(out, (j * W + t) * VE, H, dw[j]);
         }
     }
 }

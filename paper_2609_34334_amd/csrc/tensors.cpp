@@ -106,7 +106,7 @@ PyObject *read(PyObject *, PyObject *args) {
                          (long long)want);
             return false;
         }
-        word = (int64_t)(uintptr_t)t.const_data_ptr();
+        word = (int64_t)(uintptr_t)t.mutable_data_ptr();
         return true;
     });
 }

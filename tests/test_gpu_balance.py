@@ -239,8 +239,10 @@ def test_views_and_guards():
         check([x], [e], 5, out, [whole[3:3 + T * E].view(T, E)])
 
 
-def test_budgets_and_streams_give_the_same_bits():
-    xs, es = zip(*[batch(70 + b, 3000 - 500 * b, 48, 6, padding=0.1) for b in range(3)])
+@pytest.mark.parametrize("T", [60, 3000])
+def test_budgets_and_streams_give_the_same_bits(T):
+    """Batches of a workgroup each, and of many."""
+    xs, es = zip(*[batch(70 + b, T - T // 6 * b, 48, 6, padding=0.1) for b in range(3)])
     xs, es = list(xs), list(es)
     runs = []
     for wg, own in ((0, False), (1, False), (4, True), (0, True)):
@@ -257,8 +259,9 @@ def test_budgets_and_streams_give_the_same_bits():
             assert torch.equal(a, b)
 
 
-def test_replays():
-    x, e = batch(80, 900, 64, 6, padding=0.1)
+@pytest.mark.parametrize("T", [90, 900])
+def test_replays(T):
+    x, e = batch(80, T, 64, 6, padding=0.1)
     g = torch.ones(1, device="cuda")
     hc.init()
     torch.cuda.synchronize()
@@ -267,7 +270,7 @@ def test_replays():
         out = hc.balance_loss([x], [e], 8, **WEIGHTS)
         d = hc.balance_loss_backward([x], [e], out.coef, g)
     for k in range(3):
-        y, f = batch(90 + k, 900, 64, 6, padding=0.1)
+        y, f = batch(90 + k, T, 64, 6, padding=0.1)
         x.copy_(y)
         e.copy_(f)
         g.fill_(1.0 + k)

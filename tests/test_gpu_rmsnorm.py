@@ -79,8 +79,8 @@ def check_8bit(x, r, w, q, scale, h, eps=1e-6):
     assert ((q.double() * each - want).abs() <= 2.0 ** -4 * want.abs() + 2.0 ** -10 * each + 2 * err * want.abs()).all()
 
 
-# Hidden sizes around the changes of shape: a wave a row, 256 and 1024 threads; odd ones.
-HIDDEN = [1, 7, 64, 127, 130, 512, 513, 1024, 1025, 2048, 2049, 4096, 5003, 8192, 8193, 16384, 16390, 32767, 32768]
+# Hidden sizes around the changes of shape: 8 to 64 lanes a row, a workgroup a row, several vectors a thread; odd ones.
+HIDDEN = [1, 3, 7, 9, 32, 33, 64, 100, 127, 128, 130, 250, 256, 257, 384, 512, 513, 1024, 1025, 2048, 2049, 4096, 5003, 8192, 8193, 16384, 16390, 32767, 32768]
 
 
 @pytest.mark.parametrize("dt", ["bf16", "fp32"])
@@ -254,7 +254,21 @@ def test_zeros_and_what_is_not_finite():
     assert torch.isfinite(s[3]).all() and (q[3].float() == 448).all()
 
 
-@pytest.mark.parametrize("hidden", [100, 3000, 20000])
+def test_large_calls():
+    """Calls of more bytes than the caches hold, whole and ragged rows."""
+    for rows, H in ((70_001, 1024), (70_001, 1001)):
+        x, r = (tensor(i, rows, H, dt=torch.bfloat16) for i in (1, 2))
+        w = tensor(3, H)
+        y, h = hc.rmsnorm(x, w, r)
+        (q, s), h2 = hc.rmsnorm(x, w, r, quantize=True)
+        assert torch.equal(h, h2)
+        for at in (slice(0, 500), slice(rows - 500, rows)):
+            check_forward(x[at], r[at], w, y[at], h[at])
+            check_8bit(x[at], r[at], w, q[at], s[at], h[at])
+        assert torch.equal(y[1000:3000], hc.rmsnorm(x[1000:3000], w, r[1000:3000])[0])
+
+
+@pytest.mark.parametrize("hidden", [40, 100, 2500, 20000])
 def test_budgets_and_streams_give_the_same_bits(hidden):
     rows, t = 700, torch.bfloat16
     x, r, dy = (tensor(i, rows, hidden, dt=t) for i in (1, 2, 3))
@@ -275,8 +289,9 @@ def test_budgets_and_streams_give_the_same_bits(hidden):
             assert torch.equal(a, b)
 
 
-def test_replays():
-    rows, H, t = 300, 2100, torch.bfloat16
+@pytest.mark.parametrize("H", [90, 2100, 20000])
+def test_replays(H):
+    rows, t = 300, torch.bfloat16
     x, r, dy = (tensor(i, rows, H, dt=t) for i in (1, 2, 3))
     w = tensor(4, H)
     hc.init()
