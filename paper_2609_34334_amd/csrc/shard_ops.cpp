@@ -280,7 +280,7 @@ hoccl_status_t check_balance(const hoccl_balance_t *op, const size_t *tokens, in
 
 size_t balance_workspace(const hoccl_balance_t &o, const size_t *tokens, int batches) {
     uint32_t first[kMaxBatches + 1];
-    balance_blocks(tokens, o.experts, batches, first);
+    balance_blocks(tokens, o.experts, o.logits_dtype, batches, first);
     return (size_t)first[batches] * (size_t)balance_columns(o.experts, o.ranks) * 4;
 }
 
@@ -331,7 +331,7 @@ hoccl_status_t balance_loss(const void *const *logits, const void *const *choice
     TRY(mem.add(coef, nb * (size_t)o.experts * 4, 4, true, "coef"));
     TRY(mem.add(workspace, need, 4, true, "workspace"));
     TRY(mem.check());
-    balance_blocks(tokens, o.experts, batches, a.first);
+    balance_blocks(tokens, o.experts, o.logits_dtype, batches, a.first);
     a.partial = (int32_t *)workspace;
     a.loss = loss, a.expert_tokens = expert_tokens, a.rank_tokens = rank_tokens, a.coef = coef;
 
@@ -366,7 +366,7 @@ hoccl_status_t balance_backward(const void *const *logits, const void *const *ch
         TRY(mem.add(dlogits[b], n, es, true, "dlogits", b));
         a.seg[b].dlogits = dlogits[b];
         bytes += n;
-        blocks += balance_backward_blocks(tokens[b], o.experts);
+        blocks += balance_backward_blocks(tokens[b], o.experts, o.logits_dtype);
         a.first[b + 1] = (uint32_t)blocks;
     }
     TRY(mem.check());
