@@ -133,17 +133,17 @@ struct Logits {
 #pragma unroll
             for (int i = 0; i < VE; ++i) top = fmaxf(top, v[j][i]);
         top = join_lanes<L, LaneMax>(top);
-        if (fabsf(top) <= 1e38f) {
-            // In one step; the rounding of top log2 e is the same factor for
-            // all and goes with the sum.
+        if (fabsf(top) <= 65536.0f) {
+            // In one step; the rounding of top log2 e (2^-8 at most) is the
+            // same factor for all and goes with the sum.
             const float base = -top * kLog2e;
 #pragma unroll
             for (int j = 0; j < NV; ++j)
 #pragma unroll
                 for (int i = 0; i < VE; ++i) v[j][i] = __builtin_amdgcn_exp2f(fmaf(v[j][i], kLog2e, base));
         } else {
-            // All -inf: -inf - 0 leaves p = 0.  Others as large: the product
-            // with log2 e would overflow.
+            // All -inf: -inf - 0 leaves p = 0.  Others as large: that factor
+            // would leave fp32's range from 2^30 on.
             const float base = top == -INFINITY ? 0.0f : top;
 #pragma unroll
             for (int j = 0; j < NV; ++j)

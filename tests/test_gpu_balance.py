@@ -194,6 +194,25 @@ def test_masked_experts_and_padding_that_holds_anything():
         assert torch.isnan(out.loss).all()
 
 
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("E", [16, 200, 600])
+def test_logits_far_from_zero(E, dt):
+    """Rows around levels up to the types' ends, of either sign: only the
+    differences count."""
+    levels = [6.5e4, 6.6e4, 1e6, 2.0 ** 30, 1e10, 1e20, 1e30, 1e38, 3e38]
+    x, e = batch(E, 8 * len(levels), E, 3, dt)
+    for i, level in enumerate(levels):
+        for j, sign in enumerate((1.0, -1.0)):
+            t = 8 * i + 4 * j
+            x[t:t + 2] = (x[t:t + 2].float() + sign * level).to(dt)
+            x[t + 2] = sign * level
+            x[t + 3, ::2], x[t + 3, 1::2] = sign * level, -level
+    out = hc.balance_loss([x], [e], 4, **WEIGHTS)
+    (d,) = hc.balance_loss_backward([x], [e], out.coef)
+    assert torch.isfinite(out.loss).all()
+    check([x], [e], 4, out, [d])
+
+
 def test_choices_that_are_no_expert():
     x, e = batch(1, 8, 16, 3)
     e[0] = torch.tensor([2, 2, 2])                            # the same expert three times: three choices, one token
