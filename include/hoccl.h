@@ -596,7 +596,7 @@ typedef struct {
  * largest follows its gradients, the others follow in such steps.  bf16
  * parameters are rounded likewise (2^-9): small updates need fp32
  * parameters, whose bf16 `copy` is then what the all-gather sends.  eps is 0
- * or at least 2^-126.  Tensors of no elements are skipped; 48 tensors share
+ * or at least 2^-126.  Tensors of no elements are skipped; 76 tensors share
  * a launch. */
 hoccl_status_t hoccl_adamw(const hoccl_adamw_tensor_t *tensors, int count, const hoccl_adamw_t *options,
                            hipStream_t stream);

@@ -10,7 +10,6 @@ C ABI declared in ``include/hoccl.h``.
 Importing fails loudly when the library has not been built: there is no
 fallback implementation.
 """
-import array
 import collections
 import contextlib
 import ctypes
@@ -647,24 +646,11 @@ def adamw(params, grads, exp_avgs, exp_avg_sqs, exp_avg_scales=None, exp_avg_sq_
     if pdt not in _FLOATS or gdt not in _FLOATS:
         raise TypeError(f"params and grads must be fp32 or bf16, not {pdt} and {gdt}")
     states = torch.float8_e4m3fn if eight else torch.float32
-    numels = _tensors.numels(params)
-    counts = array.array("Q", numels)
-    rows = array.array("Q", bytes(64 * n))       # hoccl_adamw_tensor_t: eight words
-
-    def column(word, name, ts, dtype, numels):
-        rows[word::8] = array.array("Q", _tensors.read(name, ts, dtype, index, numels))
-
-    column(0, "params", params, pdt, numels)
-    column(1, "grads", grads, gdt, numels)
-    column(2, "exp_avgs", exp_avgs, states, numels)
-    column(3, "exp_avg_sqs", exp_avg_sqs, states, numels)
-    if eight:
-        blocks = array.array("Q", [(k + BLOCK - 1) // BLOCK for k in counts]).tobytes()
-        column(4, "exp_avg_scales", exp_avg_scales, torch.float32, blocks)
-        column(5, "exp_avg_sq_scales", exp_avg_sq_scales, torch.float32, blocks)
-    if copies is not None:
-        column(6, "copies", copies, torch.bfloat16, numels)
-    rows[7::8] = counts
+    rows = _tensors.table(index, ("params", params, pdt, 1), ("grads", grads, gdt, 1),
+                          ("exp_avgs", exp_avgs, states, 1), ("exp_avg_sqs", exp_avg_sqs, states, 1),
+                          ("exp_avg_scales", exp_avg_scales, torch.float32, BLOCK) if eight else None,
+                          ("exp_avg_sq_scales", exp_avg_sq_scales, torch.float32, BLOCK) if eight else None,
+                          None if copies is None else ("copies", copies, torch.bfloat16, 1))
     with _at(index, stream):
         o = _AdamW(_FLOATS[pdt], _FLOATS[gdt], 8 if eight else 32, 0, 0.0, betas[0], betas[1], eps, weight_decay)
         if isinstance(step, torch.Tensor):
@@ -677,7 +663,7 @@ def adamw(params, grads, exp_avgs, exp_avg_sqs, exp_avg_scales=None, exp_avg_sq_
             o.lr = lr
         if grad_scale is not None:
             o.grad_scale = _scalar(grad_scale, "grad_scale", index, torch.float32)
-        _check(_lib.hoccl_adamw(rows.buffer_info()[0], n, ctypes.byref(o), _handle(index, stream)), "hoccl_adamw")
+        _check(_lib.hoccl_adamw(rows, len(rows) // 64, ctypes.byref(o), _handle(index, stream)), "hoccl_adamw")
     return params
 
 

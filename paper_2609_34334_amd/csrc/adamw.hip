@@ -81,7 +81,7 @@ __device__ __forceinline__ void store(void *p, uint64_t e, uint64_t n, const flo
 // scales: every lane of a quad makes those of one block and gives the result
 // to the other three.
 template <bool FULL>
-__device__ __forceinline__ void put_blocks(const AdamSeg &s, uint64_t base, uint64_t n, const float (&m)[2][kVE],
+__device__ __forceinline__ void put_blocks(const AdamTensor &s, uint64_t base, uint64_t n, const float (&m)[2][kVE],
                                            const float (&r)[2][kVE]) {
     constexpr int L = kBlock / kVE;
     const uint32_t q = threadIdx.x % 4;
@@ -122,7 +122,7 @@ __device__ __forceinline__ void put_blocks(const AdamSeg &s, uint64_t base, uint
 
 // FULL: the tile ends before the tensor does.
 template <class TP, class TG, bool Q8, bool FULL>
-__device__ __forceinline__ void tile(const AdamSeg &s, const Hyper &h, uint64_t base) {
+__device__ __forceinline__ void tile(const AdamTensor &s, const Hyper &h, uint64_t base) {
     constexpr int U = kU<Q8>;
     const uint64_t n = FULL ? base + kTile<Q8> : s.n;
     float p[U][kVE], g[U][kVE], m[U][kVE], v[U][kVE];
@@ -185,6 +185,12 @@ __device__ __forceinline__ void tile(const AdamSeg &s, const Hyper &h, uint64_t 
     if constexpr (Q8) put_blocks<FULL>(s, base, n, m, r);
 }
 
+__device__ __forceinline__ AdamTensor tensor_of(const AdamSeg &s) {
+    auto word = [&](int i) { return (uint64_t)(s.hi[i / 2] >> i % 2 * 16 & 0xffff) << 32 | s.lo[i]; };
+    return {(void *)word(0),  (const void *)word(1), (void *)word(2), (void *)word(3),
+            (float *)word(4), (float *)word(5),      (void *)word(6), word(7)};
+}
+
 template <class TP, class TG, bool Q8, int CAP>
 __global__ void __launch_bounds__(kOpThreads) adamw_kernel(AdamArgsT<CAP>) {
     const AdamArgsT<CAP> &a = kernel_args<AdamArgsT<CAP>>();
@@ -201,11 +207,15 @@ __global__ void __launch_bounds__(kOpThreads) adamw_kernel(AdamArgsT<CAP>) {
     }
     const uint32_t tiles = a.first[a.nseg];
     for (uint32_t t = blockIdx.x; t < tiles; t += gridDim.x) {
-        // Lane i looks at tensor i: one read of the table, where a search
-        // would wait for six.
-        const uint32_t i = threadIdx.x % 64;
-        const int seg = __popcll(__ballot(i < (uint32_t)a.nseg && a.first[i < CAP ? i : 0] <= t)) - 1;
-        const AdamSeg &s = a.seg[seg];
+        // Lane i looks at tensors i and 64 + i: one read of the table, where a
+        // search would wait for six.
+        int seg = -1;
+#pragma unroll
+        for (uint32_t part = 0; part < CAP; part += 64) {
+            const uint32_t i = part + threadIdx.x % 64;
+            seg += __popcll(__ballot(i < (uint32_t)a.nseg && a.first[i < CAP ? i : 0] <= t));
+        }
+        const AdamTensor s = tensor_of(a.seg[seg]);
         const uint64_t base = (uint64_t)(t - a.first[seg]) * kTile<Q8>;
         if (s.n - base >= kTile<Q8>) tile<TP, TG, Q8, true>(s, h, base);
         else tile<TP, TG, Q8, false>(s, h, base);

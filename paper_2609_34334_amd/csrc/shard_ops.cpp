@@ -6,6 +6,7 @@
 #include <cfloat>
 #include <cmath>
 #include <cstring>
+#include <utility>
 #include <vector>
 
 #include "call.h"
@@ -52,21 +53,27 @@ size_t size_of(hoccl_dtype_t dt) { return dt == HOCCL_BF16 ? 2 : 4; }
 // for the pairs that a call allows by not adding the second of them.
 class Operands {
 public:
-    Operands() { all_.reserve(16); }
+    explicit Operands(size_t most = 16) { all_.reserve(most); }
     // `align`: the element size.
     hoccl_status_t add(const void *p, size_t bytes, size_t align, bool written, const char *name, long index = -1) {
         if (!p && bytes) return index < 0 ? invalid("%s is NULL", name) : invalid("%s[%ld] is NULL", name, index);
         if ((uintptr_t)p % align)
             return index < 0 ? invalid("%s is not aligned to its elements", name)
                              : invalid("%s[%ld] is not aligned to its elements", name, index);
+        if (((uintptr_t)p + bytes) >> 48)
+            return index < 0 ? invalid("%s ends behind the address space", name)
+                             : invalid("%s[%ld] ends behind the address space", name, index);
         if (bytes) all_.push_back({(uintptr_t)p, (uintptr_t)p + bytes, written, name, index});
         return HOCCL_OK;
     }
     hoccl_status_t check() {
-        std::sort(all_.begin(), all_.end(), [](const Span &a, const Span &b) { return a.lo < b.lo; });
+        std::vector<Key> order(all_.size());
+        for (size_t i = 0; i < all_.size(); ++i) order[i] = {all_[i].lo, i};
+        by_address(order);
         // The furthest reach of what came before, and of what is written of it.
         const Span *any = nullptr, *out = nullptr;
-        for (const Span &s : all_) {
+        for (const Key &k : order) {
+            const Span &s = all_[k.span];
             const Span *bad = out && out->hi > s.lo ? out : s.written && any && any->hi > s.lo ? any : nullptr;
             if (bad)
                 return invalid("%s and %s overlap (%ld, %ld)", bad->name, s.name, bad->index, s.index);
@@ -83,6 +90,30 @@ private:
         const char *name;
         long index;
     };
+    struct Key {
+        uint64_t lo;
+        size_t span;
+    };
+    // Many by radix, byte by byte from the lowest, without the bytes that are
+    // the same everywhere (the 900 of 150 tensors: 9.5 us by comparisons, 6.5 so).
+    static void by_address(std::vector<Key> &keys) {
+        if (keys.size() < 64) {
+            std::sort(keys.begin(), keys.end(), [](const Key &a, const Key &b) { return a.lo < b.lo; });
+            return;
+        }
+        uint64_t differ = 0;
+        for (const Key &k : keys) differ |= k.lo ^ keys[0].lo;
+        std::vector<Key> other(keys.size());
+        for (int shift = 0; shift < 64; shift += 8) {
+            if ((differ >> shift & 0xff) == 0) continue;
+            size_t at[256] = {};
+            for (const Key &k : keys) ++at[k.lo >> shift & 0xff];
+            size_t before = 0;
+            for (size_t &n : at) before += std::exchange(n, before);
+            for (const Key &k : keys) other[at[k.lo >> shift & 0xff]++] = k;
+            keys.swap(other);
+        }
+    }
     std::vector<Span> all_;
 };
 
@@ -115,7 +146,7 @@ hoccl_status_t adamw(const hoccl_adamw_tensor_t *ts, int count, const hoccl_adam
     const size_t ps = size_of(o.param_dtype), gs = size_of(o.grad_dtype), ss = o.state_bits == 8 ? 1 : 4;
     unsigned long long bytes = 0, tiles = 0;
     const uint32_t tile = adamw_tile(o.state_bits);
-    Operands mem;
+    Operands mem(7 * (size_t)count + 3);
     for (int i = 0; i < count; ++i) {
         const hoccl_adamw_tensor_t &t = ts[i];
         if (t.n == 0) continue;
@@ -165,7 +196,7 @@ hoccl_status_t adamw(const hoccl_adamw_tensor_t *ts, int count, const hoccl_adam
         for (; i < count && a.nseg < kAdamSegs; ++i) {
             const hoccl_adamw_tensor_t &x = ts[i];
             if (x.n == 0) continue;
-            a.seg[a.nseg] = {x.param, x.grad, x.exp_avg, x.exp_avg_sq, x.exp_avg_scale, x.exp_avg_sq_scale, x.copy, x.n};
+            a.seg[a.nseg].set({x.param, x.grad, x.exp_avg, x.exp_avg_sq, x.exp_avg_scale, x.exp_avg_sq_scale, x.copy, x.n});
             a.first[a.nseg + 1] = a.first[a.nseg] + (uint32_t)((x.n + tile - 1) / tile);
             ++a.nseg;
         }

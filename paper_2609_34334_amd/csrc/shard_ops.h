@@ -16,13 +16,25 @@ constexpr int kOpThreads = 256;  // per workgroup, of every kernel but the wide 
 
 // ---- AdamW ------------------------------------------------------------------
 
-struct AdamSeg {
+struct AdamTensor {
     void *param;
     const void *grad;
     void *m, *v;
     float *m_scale, *v_scale;
     void *copy;
     uint64_t n;
+};
+// The same in 48 bits a word, which holds a user's address and any n of a call
+// (2^31 tiles): 76 tensors fit into the 4 KiB of a launch's arguments instead
+// of 60.
+struct AdamSeg {
+    uint32_t lo[8], hi[4];  // hi: bits 32 to 47 of two words each
+    void set(const AdamTensor &t) {
+        const uint64_t w[8] = {(uint64_t)t.param, (uint64_t)t.grad,    (uint64_t)t.m,    (uint64_t)t.v,
+                               (uint64_t)t.m_scale, (uint64_t)t.v_scale, (uint64_t)t.copy, t.n};
+        for (int i = 0; i < 8; ++i) lo[i] = (uint32_t)w[i];
+        for (int i = 0; i < 4; ++i) hi[i] = (uint32_t)(w[2 * i] >> 32) | (uint32_t)(w[2 * i + 1] >> 32) << 16;
+    }
 };
 
 struct AdamStep {
@@ -41,9 +53,10 @@ struct AdamArgsT {
     int nseg;
     AdamStep step;
 };
-constexpr int kAdamSegs = 48;        // 3.4 KiB of arguments
+constexpr int kAdamSegs = 76;
 constexpr int kAdamFewSegs = 8;
 using AdamArgs = AdamArgsT<kAdamSegs>;
+static_assert(sizeof(AdamArgs) <= 4096, "the arguments of a launch");
 
 uint32_t adamw_tile(int state_bits);  // elements of one tile
 hipError_t launch_adamw(const AdamArgs &a, hoccl_dtype_t param, hoccl_dtype_t grad, int state_bits, int wg,

@@ -44,7 +44,8 @@ def test_adamw_options(kw):
 @pytest.mark.parametrize("at,value,word", [(0, 0, "param[0] is NULL"), (1, 0, "grad[0]"), (2, 0, "exp_avg[0]"),
                                            (3, 0, "exp_avg_sq[0]"), (0, P + 2, "aligned"), (2, P + 16, "overlap"),
                                            (1, P, "overlap"), (3, 3 * P + 252, "overlap"), (6, 2 * P, "overlap"),
-                                           (7, (1 << 64) - 1, "fit")])
+                                           (7, (1 << 64) - 1, "fit"), (1, 1 << 48, "address space"),
+                                           (7, 1 << 47, "address space")])
 def test_adamw_tensors(at, value, word):
     row = list(ROW)
     row[at] = value
@@ -62,6 +63,12 @@ def test_adamw_lists():
     assert adamw([ROW], state_bits=8) == BAD and "exp_avg_scale[0] is NULL" in error()
     eight = (P, 2 * P, 3 * P, 4 * P, 5 * P, 6 * P, 0, 129)
     assert adamw([eight[:5] + (5 * P + 4,) + eight[6:]], state_bits=8) == BAD and "overlap" in error()
+    # many tensors, in any order, of which two share a byte
+    for count in (3, 16, 17, 200):
+        for i, at in ((0, 0), (count // 2, 3), (count - 1, 1)):
+            rows = [[P * (1 + c * 1024 + (j * 37) % count) + 4 * j for c in range(4)] + [0, 0, 0, 65] for j in range(count)]
+            rows[i][at] = rows[(i + 1) % count][2] + 256
+            assert adamw(rows) == BAD and "overlap" in error()
     # a scalar that the call writes over
     assert adamw([ROW], grad_scale=P + 8) == BAD and "overlap" in error()
 
