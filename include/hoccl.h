@@ -661,8 +661,8 @@ typedef struct {
  * rank_tokens [ranks] = s (int32; with a batch a rank, row r of rank_tokens
  * times the elements of a token is row r of the dispatch's all-to-all(v)
  * counts), and coef [experts] (fp32), (w_i - mean of w) / T, for the
- * backward call.  The workspace: hoccl_balance_workspace bytes, 4-byte
- * aligned, whose contents before and after do not matter. */
+ * backward call.  The workspace: hoccl_balance_workspace bytes (0 for small
+ * batches), 4-byte aligned, whose contents before and after do not matter. */
 hoccl_status_t hoccl_balance_workspace(const size_t *tokens, int batches, const hoccl_balance_t *options,
                                        size_t *bytes);
 hoccl_status_t hoccl_balance_loss(const void *const *logits, const void *const *choices, const size_t *tokens,

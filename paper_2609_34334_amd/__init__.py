@@ -789,14 +789,14 @@ def balance_loss(logits, experts, ranks=1, *, expert_weight=1.0, rank_weight=0.0
     with _at(index, stream):
         need, device, o_ = ctypes.c_size_t(0), logits[0].device, ctypes.byref(o)
         _check(_lib.hoccl_balance_workspace(tokens, n, o_, ctypes.byref(need)), "hoccl_balance_workspace")
-        ws = torch.empty(need.value, dtype=torch.uint8, device=device)
+        ws = torch.empty(need.value, dtype=torch.uint8, device=device) if need.value else None
         loss = torch.empty(n, dtype=torch.float32, device=device)
         counts = torch.empty(n, E, dtype=torch.int32, device=device)
         sent = torch.empty(n, ranks, dtype=torch.int32, device=device)
         coef = torch.empty(n, E, dtype=torch.float32, device=device)
         _check(_lib.hoccl_balance_loss(lp, ep, tokens, n, o_, loss.data_ptr(), counts.data_ptr(), sent.data_ptr(),
-                                       coef.data_ptr(), ws.data_ptr(), need.value, _handle(index, stream)),
-               "hoccl_balance_loss")
+                                       coef.data_ptr(), None if ws is None else ws.data_ptr(), need.value,
+                                       _handle(index, stream)), "hoccl_balance_loss")
     return BalanceLoss(loss, counts, sent, coef)
 
 

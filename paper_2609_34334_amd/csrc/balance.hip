@@ -501,7 +501,7 @@ void balance_blocks(const size_t *tokens, int E, hoccl_dtype_t dt, int batches, 
 }
 
 hipError_t launch_balance(const BalanceArgs &a, hoccl_dtype_t dt, int wg, hipStream_t s) {
-    const bool one = balance_is_one(a);
+    const bool one = balance_is_one(a.first, a.nseg);
     const void *k = with_lanes<false>(dt, a.E, [&](auto t, auto l, auto n) {
         constexpr int L = decltype(l)::value, N = decltype(n)::value;
         return one ? (const void *)balance_kernel<decltype(t), L, N, true>

@@ -312,6 +312,7 @@ hoccl_status_t check_balance(const hoccl_balance_t *op, const size_t *tokens, in
 size_t balance_workspace(const hoccl_balance_t &o, const size_t *tokens, int batches) {
     uint32_t first[kMaxBatches + 1];
     balance_blocks(tokens, o.experts, o.logits_dtype, batches, first);
+    if (balance_is_one(first, batches)) return 0;
     return (size_t)first[batches] * (size_t)balance_columns(o.experts, o.ranks) * 4;
 }
 
@@ -370,7 +371,7 @@ hoccl_status_t balance_loss(const void *const *logits, const void *const *choice
     TRY(call.open(stream));
     const int wg = call.budget(a.first[batches]);
     TRY(call.launch(wg, [&] { return launch_balance(a, o.logits_dtype, wg, stream); }));
-    if (!balance_is_one(a)) {
+    if (!balance_is_one(a.first, batches)) {
         const int fwg = call.budget((unsigned long long)batches);
         TRY(call.launch(fwg, [&] { return launch_balance_finish(a, fwg, stream); }));
     }

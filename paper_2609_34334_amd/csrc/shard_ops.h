@@ -132,8 +132,9 @@ constexpr int balance_columns(int E, int D) { return (2 * E + D + 1 + 3) & ~3; }
 // Fills first[0 .. batches] with the blocks of the forward pass, a division
 // that goes by the sizes alone.
 void balance_blocks(const size_t *tokens, int E, hoccl_dtype_t dt, int batches, uint32_t *first);
-// Whether every batch is one workgroup's: it then finishes it as well.
-inline bool balance_is_one(const BalanceArgs &a) { return a.first[a.nseg] == (uint32_t)a.nseg; }
+// Whether every batch is one workgroup's: it then finishes it as well, and
+// needs no workspace.
+inline bool balance_is_one(const uint32_t *first, int batches) { return first[batches] == (uint32_t)batches; }
 hipError_t launch_balance(const BalanceArgs &a, hoccl_dtype_t dt, int wg, hipStream_t s);
 hipError_t launch_balance_finish(const BalanceArgs &a, int wg, hipStream_t s);
 uint32_t balance_backward_blocks(size_t tokens, int E, hoccl_dtype_t dt);

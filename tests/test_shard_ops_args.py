@@ -175,7 +175,7 @@ def options(**kw):
     return hc._Balance(**o)
 
 
-def balance(o, tokens=(16,), logits=(P,), choices=(2 * P,), loss=3 * P, n=4 * P, s=5 * P, coef=6 * P, ws=7 * P,
+def balance(o, tokens=(20000,), logits=(P,), choices=(2 * P,), loss=3 * P, n=4 * P, s=5 * P, coef=6 * P, ws=7 * P,
             size=1 << 19):
     b = len(tokens)
     vp = ctypes.c_void_p * max(1, b)
@@ -201,6 +201,15 @@ def test_balance_options(kw):
 def test_balance_arguments(kw):
     assert balance(options(), **kw) == BAD
     assert error()
+
+
+def test_balance_workspace():
+    n = ctypes.c_size_t()
+    for tokens, some in ((16, False), (20000, True)):
+        assert L.hoccl_balance_workspace((ctypes.c_size_t * 1)(tokens), 1, ctypes.byref(options()), ctypes.byref(n)) == OK
+        assert (n.value > 0) == some and n.value % 4 == 0
+    assert L.hoccl_balance_workspace(None, 1, ctypes.byref(options()), ctypes.byref(n)) == BAD
+    assert L.hoccl_balance_workspace((ctypes.c_size_t * 1)(16), 1, ctypes.byref(options()), None) == BAD
 
 
 @pytest.mark.parametrize("coef,dlogits", [(0, 4 * P), (3 * P, 0), (3 * P, P), (3 * P, 2 * P), (3 * P, 3 * P), (3 * P, 4 * P + 2)])
