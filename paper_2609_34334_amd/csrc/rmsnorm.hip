@@ -67,6 +67,9 @@ struct Shaped {
     static constexpr bool ahead = N <= 8, lean = NV >= 4, keep_weights = N <= 16;
     Raw<16> v[NV];
     // W threads a row, of which this is number t.
+    // Lines that two rows or two vectors share are read twice: through the
+    // caches, whatever NT says (the gradients of 64 MB of 5003 bf16 80 us past
+    // them and 63 so, the norm of 2049 65 and 52).
     template <bool NT>
     __device__ __forceinline__ void load(const void *p, uint64_t row, uint32_t H, uint32_t W, uint32_t t) {
         const char *at = (const char *)p + row * H * T::size;
@@ -74,7 +77,7 @@ struct Shaped {
         for (int j = 0; j < NV; ++j) {
             const uint32_t e = (j * W + t) * VE;
             if constexpr (FULL) load_raw<NT>(v[j], at + e * T::size);
-            else load_window<T, NT>(at, e, H, v[j]);
+            else load_window<T>(at, e, H, v[j]);
         }
     }
     __device__ __forceinline__ void settle(uint32_t H, uint32_t W, uint32_t t) {
@@ -398,10 +401,11 @@ constexpr unsigned long long kCacheBytes = 256ull << 20;
 constexpr unsigned kForwardThreads = 2048;
 // Workgroups of the backward pass, and partial sums: as many for each of 256
 // CUs as make about 512 threads.  16384 x 4096 takes 92 us so and 99 with 1024
-// threads; but rows whose last vectors are not whole leave lanes idle and wait
-// more (640 bf16: 2.65 TB/s with 512, 3.95 with 1024).
+// threads; but rows under 512 threads whose last vectors are not whole leave
+// lanes idle and wait more (64 MB of 640 bf16: 79 us with 512, 60 with 1024;
+// of 5003, 640 threads, 60.5 and 63.5).
 size_t backward_groups(Shape s) {
-    const int most = s.full ? 512 : 1024, threads = group_of(s);
+    const int threads = group_of(s), most = s.full || threads >= 512 ? 512 : 1024;
     return 256 * (size_t)std::max(1, (most + threads / 2) / threads);
 }
 
