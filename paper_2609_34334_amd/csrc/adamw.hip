@@ -19,7 +19,9 @@
 // states are those of the formulas taken one operation at a time in fp32.
 //
 // Bound by memory: 28 bytes an element (fp32 parameters and states, bf16
-// gradients and copies), 16.1 with 8-bit states.
+// gradients and copies; 25.2M elements in 118 us, 5.95 TB/s), 16.1 with 8-bit
+// states (63 us, 6.5 TB/s, part of it from the caches).  Many small tensors
+// are bound by the launches, of kAdamSegs tensors each, and by the host.
 #include <algorithm>
 #include <type_traits>
 

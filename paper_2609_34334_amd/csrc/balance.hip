@@ -27,8 +27,11 @@
 // of the workgroups, a number that goes by the sizes alone, are added in order
 // by one workgroup a batch.
 //
-// Bound by memory at many tokens (logits and choices read once, gradients
-// written), by the launches and the last sum's latency at few.
+// Memory's part is logits and choices read once and gradients written; what
+// holds the forward pass at many tokens is its arithmetic as well, some 8
+// instructions a logit (eight batches of 9,800 to 32,768 tokens, 256 experts,
+// bf16: 27 us for 93 MB and 9 for the sums' end, backward 29 us for 180 MB),
+// at few tokens the launches and the latency of the last sum.
 #include <algorithm>
 #include <type_traits>
 
@@ -47,9 +50,12 @@ constexpr int kAhead = 2;      // tokens of a lane in flight
 // to 32,768 tokens, 256 experts: 51 us with as many workgroups for each).
 constexpr size_t kBlocks = 512;
 // Batches of no more passes than this are a workgroup's each, which finishes
-// its batch without a second kernel: 256 tokens and 64 experts take 7.1 us
-// instead of 8.9, but 512 tokens, four passes, 10.0 instead of 8.9.
-constexpr size_t kOnePasses = 2;
+// its batch without a second kernel.  256 tokens and 64 experts, two passes,
+// take 7.1 us instead of 8.9; 512 tokens, four, 10.0 instead of 8.9, but calls
+// this short wait for the host, which a launch and a workspace less spare
+// more (both directions: eager 20 us instead of 25, replayed 14.4 instead of
+// 12.4).
+constexpr size_t kOnePasses = 4;
 constexpr float kLog2e = 1.4426950408889634f;
 
 // Logits of a lane.  16 leave fewer lanes to exchange with but more registers

@@ -21,19 +21,22 @@
 // vector a thread keeps the registers few and the waves many: with up to four
 // (256 threads for 4096 elements, one wave for 2048) the norm of 8192 x 4096
 // took 58 us instead of 47, of 4096 x 2048 into 8 bits 23.5 instead of 17, the
-// gradients at 16384 x 4096 164 instead of 117; reading ahead brought these to
-// 46, 17 and 104.  Sums are in fp32, in an order that goes by the row's length
-// alone.
+// gradients at 16384 x 4096 164 instead of 117; with the reads ahead and what
+// follows these are 42, 11 and 85 now.  Sums are in fp32, in an order that
+// goes by the row's length alone.
 //
-// The backward pass reads and writes past the caches (105 us otherwise, 94 so,
-// at 16384 x 4096); the forward pass writes past them (4096 x 2048 into 8 bits
-// 12.5 and 11.5 us, 8192 x 4096 50.8 and 50.0).  It reads through them, as its
-// inputs have mostly just been made, but where the call moves more than the
-// 256 MB that the last of them holds: 8192 x 4096 takes 43 us instead of 50,
-// 4096 x 2048, 59 MB, would take 12.7 instead of 11.1.
+// Where rows fill their last vectors the backward pass reads and writes past
+// the caches (105 us otherwise, 94 so, at 16384 x 4096).  The forward pass
+// writes past them (4096 x 2048 into 8 bits 12.5 and 11.5 us, 8192 x 4096 50.8
+// and 50.0); it reads through them, as its inputs have mostly just been made,
+// but where the call moves more than the 256 MB that the last of them holds:
+// 8192 x 4096 takes 43 us instead of 50, 4096 x 2048, 59 MB, would take 12.7
+// instead of 11.1.
 //
-// Bound by memory: 8 bytes an element (bf16 with a residual), 7 with y in 8
-// bits; backward 8 bytes and the partial sums of the weight's gradient.
+// Bound by memory: 8 bytes an element (bf16 with a residual: 6.3 TB/s at 8192 x
+// 4096), 7 with y in 8 bits; backward 8 bytes (6.3 TB/s at 16384 x 4096) and the
+// partial sums of the weight's gradient.  Rows of more than 16384 fp32 do not
+// fit the registers of one workgroup and spill (1.7 to 1.9 TB/s).
 #include <algorithm>
 #include <type_traits>
 
@@ -62,8 +65,9 @@ struct Shaped {
     // Longer rows (over 8192 bf16 elements) have no registers for the next
     // one; the longest none for the weights, which they read again, nor, in the
     // backward pass, for the residual's gradient, which is read last, and the
-    // weights' gradients, which stay in LDS (1677 rows of 20000 bf16: 141 us
-    // instead of 240; but 4092 rows of 8200 97 instead of 70).
+    // weights' gradients, which stay in LDS (when they were
+    // read past the caches 1677 rows of 20000 bf16 took 141 us instead of 240,
+    // but 4092 rows of 8200 97 instead of 70).
     static constexpr bool ahead = N <= 8, lean = NV >= 4, keep_weights = N <= 16;
     Raw<16> v[NV];
     // W threads a row, of which this is number t.
@@ -126,7 +130,7 @@ __device__ __forceinline__ void row_sums(float (&v)[M], float (*red)[16][M], uin
 }
 
 // G: lanes of a row, 256 / G rows a workgroup; 0: a workgroup a row.
-// FAR: reads past the caches.
+// FAR: reads past the caches, with FULL alone.
 template <class T, int G, int NV, bool FULL, bool Q8, bool FAR>
 __global__ void __launch_bounds__(G ? kOpThreads : 1024) rmsnorm_kernel(const RmsArgs a) {
     using X = Shaped<T, NV, FULL>;
@@ -265,7 +269,7 @@ __global__ void __launch_bounds__(G ? kOpThreads : 1024) rmsnorm_backward_kernel
                 now_h.unpack(j, u);
                 now_g.unpack(j, y);
                 if (X::lean && a.dres)
-                    load_some<T, true>((const char *)a.dres + row * H * T::size, (j * W + t) * VE, H, x);
+                    load_some<T, FULL>((const char *)a.dres + row * H * T::size, (j * W + t) * VE, H, x);
                 else if (a.dres)
                     now_d.unpack(j, x);
                 if (!X::keep_weights) load_weights(a.weight, a.weight_bf16, (j * W + t) * VE, H, w[j]);
@@ -416,16 +420,16 @@ unsigned long long rmsnorm_workgroups(size_t rows, size_t hidden, hoccl_dtype_t 
 }
 
 hipError_t launch_rmsnorm(RmsArgs a, hoccl_dtype_t dt, unsigned long long bytes, int wg, hipStream_t s) {
-    const bool far = bytes > kCacheBytes;
+    const bool far = bytes > kCacheBytes;  // with FULL alone
     const Shape sh = shape_of(a.hidden, dt);
     const void *k = with_shape(dt, sh, [&](auto type, auto g, auto n, auto full) -> const void * {
         using T = decltype(type);
         constexpr int G = decltype(g)::value, NV = decltype(n)::value;
         constexpr bool FULL = decltype(full)::value;
         if (a.scale)
-            return far ? (const void *)rmsnorm_kernel<T, G, NV, FULL, true, true>
+            return far ? (const void *)rmsnorm_kernel<T, G, NV, FULL, true, FULL>
                        : (const void *)rmsnorm_kernel<T, G, NV, FULL, true, false>;
-        return far ? (const void *)rmsnorm_kernel<T, G, NV, FULL, false, true>
+        return far ? (const void *)rmsnorm_kernel<T, G, NV, FULL, false, FULL>
                    : (const void *)rmsnorm_kernel<T, G, NV, FULL, false, false>;
     });
     a.threads = (uint32_t)sh.W;
