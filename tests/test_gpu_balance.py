@@ -258,6 +258,29 @@ def test_views_and_guards():
         check([x], [e], 5, out, [whole[3:3 + T * E].view(T, E)])
 
 
+def test_offsets_past_32_bits():
+    """2.25 G logits, the same 4400 tokens 500 times: the counts are 500
+    times theirs, the loss is theirs, the gradients are a 500th of theirs."""
+    n, T, E = 500, 4400, 1024
+    x, e = batch(11, T, E, 4, torch.bfloat16, torch.int32, 0.1)
+    xs, es = x.repeat(n, 1), e.repeat(n, 1)
+    out = hc.balance_loss([xs], [es], 8, **WEIGHTS)
+    (d,) = hc.balance_loss_backward([xs], [es], out.coef)
+    r = reference(x, e, 8, **WEIGHTS)
+    assert torch.equal(out.expert_tokens[0].cpu(), n * r["counts"])
+    assert torch.equal(out.rank_tokens[0].cpu(), n * r["sent"])
+    # a lane adds a token of 2048 (256 workgroups of 8 waves, a wave a token)
+    eps, adds = eps_of(x), n * T // 2048 + 20
+    assert abs(out.loss[0].double().cpu() - r["loss"]) <= (eps + adds * U) * abs(r["loss"])
+    p, c = r["p"], r["coef"] / n
+    dot, around = (p * c).sum(1, keepdim=True), (p * c.abs()).sum(1, keepdim=True)
+    want = p * (c - dot)
+    err = p * ((eps + 4 * U) * (c - dot).abs() + U * c.abs() + (2 * eps + 24 * U) * around) + 1e-38
+    assert ((d[-T:].double().cpu() - want).abs() <= err + 2.0 ** -8 * (want.abs() + err) + 1e-38).all()
+    for i in (0, 238, 239, 476, 477):                         # about 2^31 and 2^32 bytes, 2^31 elements
+        assert torch.equal(d[i * T:(i + 1) * T], d[-T:])
+
+
 @pytest.mark.parametrize("T", [60, 3000])
 def test_budgets_and_streams_give_the_same_bits(T):
     """Batches of a workgroup each, and of many."""

@@ -1,6 +1,7 @@
 """The operators on a rank's shard between the collectives they belong to:
 a sharded data-parallel step, the norm of sequence parallelism and an
 expert-parallel dispatch, over virtual ranks."""
+import concurrent.futures
 import math
 
 import pytest
@@ -127,3 +128,30 @@ def test_expert_parallel_dispatch():
         # tokens' softmax to about 100 roundings each, of terms as large as the loss over the tokens
         assert abs(loss.double() - want) <= 300 * U * want
         assert ((g.double() - z.grad).abs() <= 300 * U * float(want.detach()) / T).all()
+
+
+def test_threads_with_streams_of_their_own():
+    """Four host threads call the operators at once, each on its own stream
+    and tensors: the results are those of one after another."""
+    def work(seed, stream):
+        x, r, w = randn(seed, 300, 1000, dt=torch.bfloat16), randn(seed + 1, 300, 1000, dt=torch.bfloat16), randn(seed + 2, 1000)
+        p, g = [randn(seed + k, 700 * k + 1) for k in range(1, 20)], [randn(seed - k, 700 * k + 1) for k in range(1, 20)]
+        logits = [randn(seed + 7, 900, 64), randn(seed + 8, 333, 64)]
+        experts = [t.topk(4, -1).indices for t in logits]
+        states = hc.adamw_state(p, bits=8)
+        torch.cuda.synchronize()
+        for step in range(1, 21):
+            y, h = hc.rmsnorm(x, w, r, stream=stream)
+            dx, dw = hc.rmsnorm_backward(y, h, w, stream=stream)
+            hc.adamw(p, g, *states, step=step, lr=1e-2, stream=stream)
+            b = hc.balance_loss(logits, experts, 8, rank_weight=0.1, stream=stream)
+            d = hc.balance_loss_backward(logits, experts, b.coef, stream=stream)
+        stream.synchronize()
+        return [y, h, dx, dw, *p, *(t.view(torch.uint8) for s in states[:2] for t in s), *b, *d]
+
+    seeds = [1000, 2000, 3000, 4000]
+    alone = [work(s, torch.cuda.Stream()) for s in seeds]
+    with concurrent.futures.ThreadPoolExecutor(len(seeds)) as pool:
+        together = list(pool.map(lambda s: work(s, torch.cuda.Stream()), seeds))
+    for a, b in zip(alone, together):
+        assert all(torch.equal(x, y) for x, y in zip(a, b))
