@@ -33,13 +33,17 @@
 namespace hoccl {
 namespace {
 
-constexpr int kVE = 4;  // elements of a lane's vector: 32 lanes hold a block
-// Vectors of a thread in a tile.  25.2M elements: 32 bits 114 us with one, 119
-// with two; 8 bits, where two share the work on their scales, 82 and 77.
+// Elements of a lane's vector, and vectors of a thread in a tile.  25.2M
+// elements: 32 bits 114 us with one vector of four, 119 with two; 8 bits, where
+// two share the work on their scales, 82 and 77.  With bf16 parameters one of
+// eight makes wider accesses: 49 us instead of 52, but 65 instead of 59 with
+// fp32 ones, whose 32 bytes a lane are two accesses with gaps.
+template <class TP, bool Q8>
+constexpr int kVE = Q8 && TP::size == 2 ? 8 : 4;
+template <class TP, bool Q8>
+constexpr int kU = Q8 ? 8 / kVE<TP, Q8> : 1;
 template <bool Q8>
-constexpr int kU = Q8 ? 2 : 1;
-template <bool Q8>
-constexpr uint32_t kTile = kOpThreads * kVE * kU<Q8>;
+constexpr uint32_t kTile = kOpThreads * (Q8 ? 8 : 4);
 
 // Every byte is used once a step: reads and writes are non-temporal.  With
 // plain ones 25.2M elements took 136 us instead of 119 (32 bits).  The codes
@@ -67,47 +71,52 @@ __device__ __forceinline__ void load(const void *p, uint64_t e, uint64_t n, Raw<
     if constexpr (FULL) load_raw<NT>(r, (const char *)p + e * T::size);
     else load_window<T, NT>(p, e, n, r);
 }
-template <class T, bool FULL>
-__device__ __forceinline__ void store(void *p, uint64_t e, uint64_t n, const float (&f)[kVE]) {
+template <class T, bool FULL, int VE>
+__device__ __forceinline__ void store(void *p, uint64_t e, uint64_t n, const float (&f)[VE]) {
     if constexpr (FULL) {
-        Raw<T::size * kVE> r;
-        T::template pack<kVE>(f, r);
+        Raw<T::size * VE> r;
+        T::template pack<VE>(f, r);
         store_raw<kNT>((char *)p + e * T::size, r);
     } else {
         store_some<T, kNT>(p, e, n, f);
     }
 }
 
-// The two vectors' moments as e4m3 bytes and scales.  The four blocks that 32
-// lanes hold (m and the root of v, twice) share the divisions for their
-// scales: every lane of a quad makes those of one block and gives the result
-// to the other three.
-template <bool FULL>
-__device__ __forceinline__ void put_blocks(const AdamTensor &s, uint64_t base, uint64_t n, const float (&m)[2][kVE],
-                                           const float (&r)[2][kVE]) {
-    constexpr int L = kBlock / kVE;
-    const uint32_t q = threadIdx.x % 4;
-    uint32_t top[4];
+// The vectors' moments as e4m3 bytes and scales.  The blocks that a block's
+// lanes hold (m and the root of v, once or twice) share the divisions for their
+// scales: of neighbouring lanes each makes those of one block and gives the
+// result to the others.
+template <bool FULL, int U, int VE>
+__device__ __forceinline__ void put_blocks(const AdamTensor &s, uint64_t base, uint64_t n, const float (&m)[U][VE],
+                                           const float (&r)[U][VE]) {
+    constexpr int L = kBlock / VE, N = 2 * U;
+    const uint32_t q = threadIdx.x % N;
+    uint32_t top[N];
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
+    for (int u = 0; u < U; ++u) {
         top[2 * u] = join_lanes<L, LaneUMax>(top_bits(m[u]));
         top[2 * u + 1] = join_lanes<L, LaneUMax>(top_bits(r[u]));
     }
-    float scale, mine;
-    block_scale(__uint_as_float(q < 2 ? (q == 0 ? top[0] : top[1]) : (q == 2 ? top[2] : top[3])), scale, mine);
-    const float inv[4] = {dpp<0x00>(mine), dpp<0x55>(mine), dpp<0xAA>(mine), dpp<0xFF>(mine)};
+    float scale, mine, inv[N];
+    if constexpr (U == 2) {
+        block_scale(__uint_as_float(q < 2 ? (q == 0 ? top[0] : top[1]) : (q == 2 ? top[2] : top[3])), scale, mine);
+        inv[0] = dpp<0x00>(mine), inv[1] = dpp<0x55>(mine), inv[2] = dpp<0xAA>(mine), inv[3] = dpp<0xFF>(mine);
+    } else {
+        block_scale(__uint_as_float(q == 0 ? top[0] : top[1]), scale, mine);
+        inv[0] = dpp<0xA0>(mine), inv[1] = dpp<0xF5>(mine);  // quad_perm 0,0,2,2 and 1,1,3,3
+    }
 #pragma unroll
-    for (int u = 0; u < 2; ++u) {
-        const uint64_t e = base + (uint64_t)(u * kOpThreads + threadIdx.x) * kVE;
-        float x[kVE], y[kVE];
+    for (int u = 0; u < U; ++u) {
+        const uint64_t e = base + (uint64_t)(u * kOpThreads + threadIdx.x) * VE;
+        float x[VE], y[VE];
 #pragma unroll
-        for (int i = 0; i < kVE; ++i) {
+        for (int i = 0; i < VE; ++i) {
             x[i] = m[u][i] * inv[2 * u];
             y[i] = r[u][i] * inv[2 * u + 1];
             // A root that is not zero is not held as zero.
             y[i] = y[i] > 0.0f && y[i] < kLeast ? kLeast : y[i];
         }
-        Raw<kVE> a, b;
+        Raw<VE> a, b;
         to_e4m3(x, a);
         to_e4m3(y, b);
         if constexpr (FULL) {
@@ -118,24 +127,24 @@ __device__ __forceinline__ void put_blocks(const AdamTensor &s, uint64_t base, u
             store_bytes(s.v, e, n, b);
         }
     }
-    const uint64_t first = base + (uint64_t)(q / 2 * kOpThreads + threadIdx.x / L * L) * kVE;
-    if (threadIdx.x % L < 4 && (FULL || first < n)) (q % 2 ? s.v_scale : s.m_scale)[first / kBlock] = scale;
+    const uint64_t first = base + (uint64_t)(q / 2 * kOpThreads + threadIdx.x / L * L) * VE;
+    if (threadIdx.x % L < N && (FULL || first < n)) (q % 2 ? s.v_scale : s.m_scale)[first / kBlock] = scale;
 }
 
 // FULL: the tile ends before the tensor does.
 template <class TP, class TG, bool Q8, bool FULL>
 __device__ __forceinline__ void tile(const AdamTensor &s, const Hyper &h, uint64_t base) {
-    constexpr int U = kU<Q8>;
+    constexpr int U = kU<TP, Q8>, VE = kVE<TP, Q8>;
     const uint64_t n = FULL ? base + kTile<Q8> : s.n;
-    float p[U][kVE], g[U][kVE], m[U][kVE], v[U][kVE];
+    float p[U][VE], g[U][VE], m[U][VE], v[U][VE];
     using TS = std::conditional_t<Q8, EByte, EF32>;
-    Raw<TP::size * kVE> rp[U];
-    Raw<TG::size * kVE> rg[U];
-    Raw<TS::size * kVE> rm[U], rv[U];
+    Raw<TP::size * VE> rp[U];
+    Raw<TG::size * VE> rg[U];
+    Raw<TS::size * VE> rm[U], rv[U];
     float sm[U], sv[U];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const uint64_t e = base + (uint64_t)(u * kOpThreads + threadIdx.x) * kVE;
+        const uint64_t e = base + (uint64_t)(u * kOpThreads + threadIdx.x) * VE;
         load<TP, kNT, FULL>(s.param, e, n, rp[u]);
         load<TG, kNT, FULL>(s.grad, e, n, rg[u]);
         load<TS, kNT && !Q8, FULL>(s.m, e, n, rm[u]);
@@ -147,35 +156,35 @@ __device__ __forceinline__ void tile(const AdamTensor &s, const Hyper &h, uint64
     }
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const uint64_t e = base + (uint64_t)(u * kOpThreads + threadIdx.x) * kVE;
+        const uint64_t e = base + (uint64_t)(u * kOpThreads + threadIdx.x) * VE;
         if constexpr (!FULL) {
             settle_window<TP>(e, n, rp[u]);
             settle_window<TG>(e, n, rg[u]);
             settle_window<TS>(e, n, rm[u]);
             settle_window<TS>(e, n, rv[u]);
         }
-        TP::template unpack<kVE>(rp[u], p[u]);
-        TG::template unpack<kVE>(rg[u], g[u]);
+        TP::template unpack<VE>(rp[u], p[u]);
+        TG::template unpack<VE>(rg[u], g[u]);
         if constexpr (Q8) {
             from_e4m3(rm[u], m[u]);
             from_e4m3(rv[u], v[u]);
 #pragma unroll
-            for (int i = 0; i < kVE; ++i) {
+            for (int i = 0; i < VE; ++i) {
                 m[u][i] *= sm[u];
                 const float r = v[u][i] * sv[u];
                 v[u][i] = r * r;
             }
         } else {
-            EF32::unpack<kVE>(rm[u], m[u]);
-            EF32::unpack<kVE>(rv[u], v[u]);
+            EF32::unpack<VE>(rm[u], m[u]);
+            EF32::unpack<VE>(rv[u], v[u]);
         }
     }
-    float r[U][kVE];
+    float r[U][VE];
 #pragma unroll
     for (int u = 0; u < U; ++u) {
-        const uint64_t e = base + (uint64_t)(u * kOpThreads + threadIdx.x) * kVE;
+        const uint64_t e = base + (uint64_t)(u * kOpThreads + threadIdx.x) * VE;
 #pragma unroll
-        for (int i = 0; i < kVE; ++i) p[u][i] = step_one(h, p[u][i], g[u][i], m[u][i], v[u][i], r[u][i]);
+        for (int i = 0; i < VE; ++i) p[u][i] = step_one(h, p[u][i], g[u][i], m[u][i], v[u][i], r[u][i]);
         if constexpr (!Q8) {
             store<EF32, FULL>(s.m, e, n, m[u]);
             store<EF32, FULL>(s.v, e, n, v[u]);
