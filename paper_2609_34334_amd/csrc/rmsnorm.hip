@@ -35,8 +35,7 @@
 //
 // Bound by memory: 8 bytes an element (bf16 with a residual: 6.3 TB/s at 8192 x
 // 4096), 7 with y in 8 bits; backward 8 bytes (6.3 TB/s at 16384 x 4096) and the
-// partial sums of the weight's gradient.  Rows of more than 16384 fp32 do not
-// fit the registers of one workgroup and spill (1.7 to 1.9 TB/s).
+// partial sums of the weight's gradient.
 #include <algorithm>
 #include <type_traits>
 
@@ -65,10 +64,15 @@ struct Shaped {
     // Longer rows (over 8192 bf16 elements) have no registers for the next
     // one; the longest none for the weights, which they read again, nor, in the
     // backward pass, for the residual's gradient, which is read last, and the
-    // weights' gradients, which stay in LDS (when they were
-    // read past the caches 1677 rows of 20000 bf16 took 141 us instead of 240,
-    // but 4092 rows of 8200 97 instead of 70).
-    static constexpr bool ahead = N <= 8, lean = NV >= 4, keep_weights = N <= 16;
+    // weights' gradients, which stay in LDS (64 MB of 20000 bf16: 57 us instead
+    // of 124; but of 12288 fp32, whose 16 elements a thread fit, 56 instead of
+    // 48).
+    static constexpr bool ahead = N <= 8, lean = N >= 32, keep_weights = N <= 16;
+    // The offsets of many vectors, their comparisons with the row's end and their
+    // addresses would be kept over the loop, in more registers than the row
+    // (64 MB of 20000 fp32: 133 us, and the gradients 139): they are made anew
+    // for every row (49, 87), of the longest again after its sums (41, 50).
+    static constexpr bool anew = NV >= 4, again = NV >= 8;
     Raw<16> v[NV];
     // W threads a row, of which this is number t.
     // Lines that two rows or two vectors share are read twice: through the
@@ -137,7 +141,9 @@ __global__ void __launch_bounds__(G ? kOpThreads : 1024) rmsnorm_kernel(const Rm
     constexpr int VE = X::VE, ROWS = G ? kOpThreads / G : 1;
     __shared__ float red[2][16][1];
     int turn = 0;
-    const uint32_t H = a.hidden, W = G ? G : a.threads, t = G ? threadIdx.x % G : threadIdx.x;
+    const uint32_t H = a.hidden, W = G ? G : a.threads;
+    uint32_t t = G ? threadIdx.x % G : threadIdx.x;
+    if constexpr (G != 8) __builtin_assume(H >= VE);  // over 8 vectors
     const uint32_t nblk = (H + kBlock - 1) / kBlock;
     const uint64_t step = (uint64_t)gridDim.x * ROWS;
     uint64_t row = (uint64_t)blockIdx.x * ROWS + (G ? threadIdx.x / G : 0);
@@ -152,6 +158,7 @@ __global__ void __launch_bounds__(G ? kOpThreads : 1024) rmsnorm_kernel(const Rm
 #pragma unroll
         for (int j = 0; j < NV; ++j) load_weights(a.weight, a.weight_bf16, (j * W + t) * VE, H, w[j]);
     for (; row < a.rows; row += step) {
+        if constexpr (X::anew) t = here(t);
         const uint64_t at = row * H * T::size;
         float h[NV][VE], sum[1] = {0.0f};
         if (!X::ahead) load(row);
@@ -180,6 +187,7 @@ __global__ void __launch_bounds__(G ? kOpThreads : 1024) rmsnorm_kernel(const Rm
             for (int i = 0; i < VE; ++i) sum[0] += h[j][i] * h[j][i];
         }
         row_sums<G>(sum, red, W / 64, turn);
+        if constexpr (X::again) t = here(t);
         const float r = 1.0f / __builtin_sqrtf(sum[0] / (float)H + a.eps);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
@@ -219,7 +227,9 @@ __global__ void __launch_bounds__(G ? kOpThreads : 1024) rmsnorm_backward_kernel
     __shared__ float cols[G ? G * VE : 1];
     extern __shared__ float4 grads[];  // lean: a row's, each thread its own
     int turn = 0;
-    const uint32_t H = a.hidden, W = G ? G : a.threads, t = G ? threadIdx.x % G : threadIdx.x;
+    const uint32_t H = a.hidden, W = G ? G : a.threads;
+    uint32_t t = G ? threadIdx.x % G : threadIdx.x;
+    if constexpr (G != 8) __builtin_assume(H >= VE);  // over 8 vectors
     const int slot = G ? threadIdx.x / G : 0;
     const uint64_t step = (uint64_t)a.blocks * ROWS;
     X h, g, d;
@@ -240,6 +250,7 @@ __global__ void __launch_bounds__(G ? kOpThreads : 1024) rmsnorm_backward_kernel
         uint64_t row = (uint64_t)part * ROWS + slot;
         if (X::ahead && row < a.rows) load(row);
         for (; row < a.rows; row += step) {
+            if constexpr (X::anew) t = here(t);
             if (!X::ahead) load(row);
             X now_h = h, now_g = g, now_d = d;
             if (X::ahead && row + step < a.rows) load(row + step);
@@ -260,6 +271,7 @@ __global__ void __launch_bounds__(G ? kOpThreads : 1024) rmsnorm_backward_kernel
                 }
             }
             row_sums<G>(sums, red, W / 64, turn);
+            if constexpr (X::again) t = here(t);
             const float r = 1.0f / __builtin_sqrtf(sums[0] / (float)H + a.eps);
             const float c = sums[1] / (float)H * r * r;
             now_h.forget(), now_g.forget();
