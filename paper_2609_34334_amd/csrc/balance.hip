@@ -243,6 +243,7 @@ __global__ void __launch_bounds__(kThreads) balance_kernel(BalanceArgs) {
     __shared__ int sum_live;
     __shared__ double tot[ONE ? kColumns : 1];
     const int E = a.E, D = a.D, k = a.k, stride = balance_columns(E, D);
+    if constexpr (L > 1) __builtin_assume(E > N);  // over the logits of one lane
     const int lane = threadIdx.x % L, slot = threadIdx.x / L;
     for (uint32_t block = blockIdx.x; block < a.first[a.nseg]; block += gridDim.x) {
         uint32_t lb, nb;
@@ -407,6 +408,7 @@ __global__ void __launch_bounds__(kOpThreads) balance_backward_kernel(BalanceArg
     using X = Logits<T, L, N>;
     constexpr int ROWS = kOpThreads / L;
     const int E = a.E, k = a.k;
+    if constexpr (L > 1) __builtin_assume(E > N);  // over the logits of one lane
     const int lane = threadIdx.x % L, slot = threadIdx.x / L;
     for (uint32_t block = blockIdx.x; block < a.first[a.nseg]; block += gridDim.x) {
         uint32_t lb, nb;
