@@ -260,11 +260,14 @@ hoccl_status_t rmsnorm_backward(const void *dy, const void *dres, const void *h,
     if (workspace_bytes < need)
         return invalid("a workspace of %zu bytes where %zu are needed", workspace_bytes, need);
     Operands mem;
-    TRY(mem.add(dy, bytes, es, dy == dx, "dy"));
-    if (dres && dres != dy) TRY(mem.add(dres, bytes, es, dres == dx, "dresidual"));
-    if (h != dy && h != dres) TRY(mem.add(h, bytes, es, h == dx, "h"));
+    // Inputs may be the same buffer, and dx one of them; a NULL, which dres may
+    // be, is no buffer.
+    auto is = [](const void *a, const void *b) { return a && a == b; };
+    TRY(mem.add(dy, bytes, es, is(dy, dx), "dy"));
+    if (dres && !is(dres, dy)) TRY(mem.add(dres, bytes, es, is(dres, dx), "dresidual"));
+    if (!is(h, dy) && !is(h, dres)) TRY(mem.add(h, bytes, es, is(h, dx), "h"));
     TRY(mem.add(weight, hidden * size_of(wdt), size_of(wdt), false, "weight"));
-    if (dx != dy && dx != dres && dx != h) TRY(mem.add(dx, bytes, es, true, "dx"));
+    if (!is(dx, dy) && !is(dx, dres) && !is(dx, h)) TRY(mem.add(dx, bytes, es, true, "dx"));
     if (dweight) TRY(mem.add(dweight, hidden * 4, 4, true, "dweight"));
     TRY(mem.add(workspace, need, 4, true, "workspace"));
     TRY(mem.check());

@@ -136,6 +136,14 @@ def test_rmsnorm_backward_arguments(kw):
     assert error()
 
 
+@pytest.mark.parametrize("kw,word", [(dict(h=0), "h is NULL"), (dict(dx=0), "dx is NULL"), (dict(dy=0), "dy is NULL"),
+                                     (dict(h=0, dx=0), "h is NULL"), (dict(dx=0, dw=0, ws=0, size=0), "dx is NULL")])
+def test_rmsnorm_backward_without_a_residual_gradient(kw, word):
+    """No residual gradient (NULL) does not stand for another operand that is missing."""
+    assert backward(dres=0, **kw) == BAD
+    assert word in error()
+
+
 def test_rmsnorm_backward_workspace():
     n = ctypes.c_size_t()
     assert L.hoccl_rmsnorm_backward_workspace(8, 64, hc.BF16, ctypes.byref(n)) == OK and n.value >= 256
