@@ -1143,9 +1143,12 @@ hoccl_status_t OpCall::open(hipStream_t s) {
 int OpCall::cus() const { return impl_->st->num_cus; }
 
 int OpCall::budget(unsigned long long want) const {
+    // A launch has fewer than 2^32 threads, a workgroup up to 1024; the
+    // kernels stride over what is more.
+    constexpr unsigned long long kMost = (1ull << 22) - 1;
     const int most = impl_->cfg.workgroups_per_step;
-    if (most > 0 && want > (unsigned long long)most) return most;
-    return (int)std::min(std::max(want, 1ull), 1ull << 30);
+    if (most > 0) want = std::min(want, (unsigned long long)most);
+    return (int)std::min(std::max(want, 1ull), kMost);
 }
 
 hoccl_status_t OpCall::before() { return timed_begin(*impl_->st, impl_->cfg, impl_->s, &impl_->tp); }

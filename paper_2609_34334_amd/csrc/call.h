@@ -29,7 +29,7 @@ public:
     hoccl_status_t open(hipStream_t s);
     int cus() const;
     // The workgroups to launch where `want` would be the automatic choice:
-    // at most workgroups_per_step, where that is set.
+    // at most workgroups_per_step, where that is set, and what a launch takes.
     int budget(unsigned long long want) const;
     // f() enqueues one kernel on the stream and returns its hipError_t.
     template <typename F>

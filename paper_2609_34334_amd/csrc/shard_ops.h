@@ -25,7 +25,7 @@ struct AdamTensor {
     uint64_t n;
 };
 // The same in 48 bits a word, which holds a user's address and any n of a call
-// (2^31 tiles): 76 tensors fit into the 4 KiB of a launch's arguments instead
+// (fewer than 2^31 tiles): 76 tensors fit into the 4 KiB of a launch's arguments instead
 // of 60.
 struct AdamSeg {
     uint32_t lo[8], hi[4];  // hi: bits 32 to 47 of two words each

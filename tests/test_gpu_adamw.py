@@ -310,3 +310,31 @@ def test_more_than_2_to_the_32_bytes():
     assert int((m[0].view(torch.uint8) != 0).sum()) == len(at) == int((v[0].view(torch.uint8) != 0).sum())
     lit = torch.unique(idx // 128)
     assert torch.equal(torch.nonzero(ms[0]).flatten(), lit) and torch.equal(torch.nonzero(vs[0]).flatten(), lit)
+
+
+def test_more_tiles_than_a_launch_has_workgroups():
+    """2^34 elements and some, 2^24 tiles: a launch has fewer than 2^32
+    threads, so its workgroups take several tiles each."""
+    n = (1 << 34) + 1024 * 3 + 7
+    need = 12 * n + (8 << 30)
+    torch.cuda.empty_cache()
+    if torch.cuda.mem_get_info()[0] < need:
+        pytest.skip(f"needs {need >> 30} GiB of free GPU memory")
+    p, g = (torch.zeros(n, dtype=torch.bfloat16, device="cuda") for _ in range(2))
+    m, v, _, _ = hc.adamw_state([p])
+    at = [0, 1, 1023, 1024, (1 << 32) - 1, 1 << 32, (1 << 33) + 5, (1 << 34) - 1, 1 << 34, (1 << 34) + 1, n - 8, n - 2, n - 1]
+    idx = torch.tensor(at, device="cuda")
+    g[idx] = torch.arange(1, len(at) + 1, device="cuda").to(torch.bfloat16)
+    hc.adamw([p], [g], m, v, step=1, lr=0.5, weight_decay=0.0)
+    torch.cuda.synchronize()
+    stats = hc.last_stats()
+    assert stats["reduce_launches"] == 1 and stats["workgroups_per_step"] * 256 < 1 << 32
+    # The first step moves each parameter with a gradient by lr, the others not.
+    assert torch.allclose(p[idx].float(), torch.full((len(at),), -0.5, device="cuda"), atol=0.5 * BF * 1.01)
+    assert torch.allclose(m[0][idx], 0.1 * g[idx].float(), rtol=4 * U) and (v[0][idx] > 0).all()
+    near = torch.tensor([i for a in at for i in (a - 2, a + 2) if 0 <= i < n and i not in at], device="cuda")
+    assert (p[near] == 0).all() and (m[0][near] == 0).all() and (v[0][near] == 0).all()
+    # every element was stepped once: the parts of p that moved are those of the list
+    assert sum(int(torch.count_nonzero(p[i:i + (1 << 31)])) for i in range(0, n, 1 << 31)) == len(at)
+    del p, g, m, v
+    torch.cuda.empty_cache()
