@@ -633,7 +633,10 @@ def adamw(params, grads, exp_avgs, exp_avg_sqs, exp_avg_scales=None, exp_avg_sq_
     bf16 tensors that receive the new parameters.  `step` counts from 1; it
     may be an int32 tensor of one element on the GPU and `lr` an fp32 one,
     which are then read when the work runs.  `grad_scale`: an fp32 tensor of
-    one element that multiplies every gradient.  Returns `params`."""
+    one element that multiplies every gradient.  Params may require gradients:
+    like torch's own writes in place under no_grad, the step is no part of a
+    graph, and a backward pass over a graph that saved what it overwrote is
+    refused.  Returns `params`."""
     n = len(params)
     eight = exp_avg_scales is not None
     if eight != (exp_avg_sq_scales is not None):
@@ -664,6 +667,7 @@ def adamw(params, grads, exp_avgs, exp_avg_sqs, exp_avg_scales=None, exp_avg_sq_
         if grad_scale is not None:
             o.grad_scale = _scalar(grad_scale, "grad_scale", index, torch.float32)
         _check(_lib.hoccl_adamw(rows, len(rows) // 64, ctypes.byref(o), _handle(index, stream)), "hoccl_adamw")
+    _tensors.wrote(params, exp_avgs, exp_avg_sqs, exp_avg_scales, exp_avg_sq_scales, copies)
     return params
 
 
@@ -680,13 +684,18 @@ def rmsnorm(x, weight, residual=None, *, eps=1e-6, quantize=False, out=None, res
     residual, rounded to the type of x.  With `quantize` y is a pair of
     float8_e4m3fn values, shaped like x, and fp32 scales [..., blocks of
     BLOCK].  `out` (y, or the pair) and `residual_out` default to new tensors;
-    y and residual_out may each be x or residual itself."""
+    y and residual_out may each be x or residual itself.  The results are no
+    part of an autograd graph, whatever requires gradients: rmsnorm_backward
+    makes them."""
     index = x.get_device()
     dt = _want(x, "x", index, _FLOATS)
     rows, hidden = _rows(x)
     wdt = _want(weight, "weight", index, _FLOATS, (hidden,))
     if residual is not None:
         _want(residual, "residual", index, (x.dtype,), x.shape)
+    given = () if out is None else out if quantize else (out,)
+    if residual_out is not None:
+        given = (*given, residual_out)
     with _at(index, stream):
         q = scale = y = None
         if quantize:
@@ -712,6 +721,8 @@ def rmsnorm(x, weight, residual=None, *, eps=1e-6, quantize=False, out=None, res
                                       None if residual_out is None else residual_out.data_ptr(),
                                       (q if quantize else y).data_ptr(), scale.data_ptr() if quantize else None,
                                       rows, hidden, eps, dt, wdt, _handle(index, stream)), "hoccl_rmsnorm")
+            if given:
+                _tensors.wrote(given)
     y = (q, scale) if quantize else y
     return y if residual is None else (y, residual_out)
 
@@ -748,6 +759,8 @@ def rmsnorm_backward(grad, h, weight, grad_residual=None, *, eps=1e-6, weight_gr
                                                dweight.data_ptr() if weight_grad else None,
                                                ws.data_ptr() if weight_grad else None, need.value, rows, hidden, eps,
                                                dt, wdt, _handle(index, stream)), "hoccl_rmsnorm_backward")
+            if out is not None:
+                _tensors.wrote((out,))
     return dx, dweight
 
 
@@ -782,7 +795,9 @@ def balance_loss(logits, experts, ranks=1, *, expert_weight=1.0, rank_weight=0.0
     token without a choice is padding), `ranks` ranks of E / ranks experts.
     Returns a BalanceLoss: loss [batches], expert_tokens [batches, E] and
     rank_tokens [batches, ranks] (int32: choices of an expert, tokens sent to
-    a rank), and coef, which balance_loss_backward takes."""
+    a rank), and coef, which balance_loss_backward takes.  The loss is no part
+    of an autograd graph, whatever requires gradients: balance_loss_backward
+    makes them."""
     index, o, tokens, lp, ep = _balance(logits, experts, ranks, (expert_weight, rank_weight, traffic_weight),
                                         0 if max_ranks is None else max_ranks)
     n, E = len(logits), o.experts

@@ -13,6 +13,9 @@
 // elements, rounded up.  Checked like read().
 // rows(name, tensors, columns): their first sizes as bytes, once all have two
 // dimensions, the second of `columns`; ValueError otherwise.
+// wrote(*lists): the tensors of the lists (None: of none) have been written
+// through their addresses: their versions go on, as after torch's own writes,
+// so that a backward pass over a graph that saved one of them is refused.
 #define PY_SSIZE_T_CLEAN
 #include <torch/csrc/Dtype.h>
 #include <torch/csrc/autograd/python_variable.h>
@@ -170,9 +173,28 @@ PyObject *rows(PyObject *, PyObject *args) {
     });
 }
 
+PyObject *wrote(PyObject *, PyObject *args) {
+    return guarded([&]() -> PyObject * {
+        for (Py_ssize_t i = 0; i < PyTuple_GET_SIZE(args); ++i) {
+            if (PyTuple_GET_ITEM(args, i) == Py_None) continue;
+            PyObject *seq = PySequence_Fast(PyTuple_GET_ITEM(args, i), "a list of tensors is needed");
+            if (!seq) return nullptr;
+            const bool fine = each(seq, [](Py_ssize_t, const at::Tensor &t) {
+                // Those of inference mode have no version.
+                if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+                return true;
+            });
+            Py_DECREF(seq);
+            if (!fine) return nullptr;
+        }
+        Py_RETURN_NONE;
+    });
+}
+
 PyMethodDef methods[] = {{"read", (PyCFunction)read, METH_VARARGS, nullptr},
                          {"table", (PyCFunction)table, METH_VARARGS, nullptr},
                          {"rows", (PyCFunction)rows, METH_VARARGS, nullptr},
+                         {"wrote", (PyCFunction)wrote, METH_VARARGS, nullptr},
                          {nullptr, nullptr, 0, nullptr}};
 PyModuleDef module = {PyModuleDef_HEAD_INIT, "_tensors", nullptr, -1, methods, nullptr, nullptr, nullptr, nullptr};
 

@@ -262,6 +262,27 @@ def test_numbers_on_the_device_and_replays():
         del graph
 
 
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_graph_that_saved_a_parameter_is_refused(bits):
+    """The step writes in place: a backward pass that needs what it wrote
+    over is refused, as after torch's own writes in place."""
+    c = Case([300, 40], 8, bits=bits)
+    held = [t for ts in (c.p, c.m, c.v, c.ms, c.vs, c.c) if ts for t in ts]
+    leaf = c.p[0].requires_grad_()
+    loss = (leaf * leaf).sum()
+    versions = [t._version for t in held]
+    c.step()
+    assert all(t._version > v for t, v in zip(held, versions))
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()
+    (leaf * leaf).sum().backward()
+    assert torch.equal(leaf.grad, 2 * leaf.detach())
+    before = [t._version for t in held]
+    with pytest.raises(hc.HocclError):
+        hc.adamw(c.p * 2, c.g * 2, c.m * 2, c.v * 2, c.ms and c.ms * 2, c.vs and c.vs * 2, step=1, lr=0.1)
+    assert [t._version for t in held] == before           # refused: nothing written
+
+
 def test_what_is_not_finite():
     """An infinite or NaN gradient spoils its element alone with fp32 states
     and its block of 128 with 8-bit ones."""

@@ -328,3 +328,27 @@ def test_offsets_past_32_bits():
     dx, dw = hc.rmsnorm_backward(x, x, w, out=y)
     for at in (0, 65600, rows - 1):
         check_backward(x[at], x[at], None, w, dx[at], None)
+
+
+def test_outputs_that_are_given_count_as_written():
+    """A graph that saved a tensor which a call then writes is refused."""
+    x, r, w = (torch.randn(6, 40, device="cuda") for _ in range(3))
+    w = w[0].contiguous()
+    pair = (torch.empty(6, 40, dtype=torch.float8_e4m3fn, device="cuda"), torch.empty(6, 1, device="cuda"))
+    fresh = torch.empty(6, 40, device="cuda")
+    for out, call in (([fresh], lambda: hc.rmsnorm(x, w, out=fresh)),
+                      ([x, r], lambda: hc.rmsnorm(x, w, r, out=x, residual_out=r)),
+                      ([*pair, r], lambda: hc.rmsnorm(x, w, r, quantize=True, out=pair, residual_out=r)),
+                      ([fresh], lambda: hc.rmsnorm_backward(x, r, w, out=fresh)),
+                      ([], lambda: hc.rmsnorm(x, w, r)), ([], lambda: hc.rmsnorm_backward(x, r, w))):
+        every = [x, r, w, fresh, *pair]
+        versions = [t._version for t in every]
+        call()
+        for t, v in zip(every, versions):
+            assert (t._version > v) == any(t is o for o in out)
+    leaf = torch.randn(6, 40, device="cuda", requires_grad=True)
+    mid = leaf * 2
+    loss = (mid * mid).sum()
+    hc.rmsnorm(x, w, out=mid.detach())
+    with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+        loss.backward()

@@ -73,6 +73,20 @@ def test_adamw_lists():
     assert adamw([ROW], grad_scale=P + 8) == BAD and "overlap" in error()
 
 
+def test_versions_of_written_tensors():
+    """What an operator writes by address counts as written for autograd."""
+    a, b = torch.zeros(4), torch.zeros(3, requires_grad=True)
+    with torch.inference_mode():
+        c = torch.zeros(2)                                            # has no version
+    versions = a._version, b._version
+    hc._tensors.wrote([a, c], None, (b, a))
+    assert (a._version, b._version) == (versions[0] + 2, versions[1] + 1)
+    with pytest.raises(TypeError):
+        hc._tensors.wrote([a, None])
+    with pytest.raises(TypeError):
+        hc._tensors.wrote(3)
+
+
 def test_adamw_python():
     p, g = [torch.zeros(4)], [torch.zeros(4)]
     m, v, _, _ = hc.adamw_state(p)
