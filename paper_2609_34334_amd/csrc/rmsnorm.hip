@@ -133,6 +133,20 @@ __device__ __forceinline__ void row_sums(float (&v)[M], float (*red)[16][M], uin
     }
 }
 
+// 1 / sqrt(v), rounded once: the approximation (1 ulp) and a Newton step on it,
+// r + r (1 - v r r) / 2, whose difference is taken in two parts, from the
+// rounded product v r and from its rounding.  (1 / sqrtf rounds twice and takes
+// more instructions.)  Values near and in the subnormal range are scaled; of
+// infinity it is 0.
+__device__ __forceinline__ float reciprocal_root(float v) {
+    const bool tiny = v < 0x1p-100f;
+    if (tiny) v *= 0x1p100f;
+    const float r = __builtin_amdgcn_rsqf(v), h = v * r;
+    const float e = fmaf(-fmaf(v, r, -h), r, fmaf(-h, r, 1.0f));
+    const float s = v < INFINITY ? fmaf(0.5f * r, e, r) : r;
+    return tiny ? s * 0x1p50f : s;
+}
+
 // G: lanes of a row, 256 / G rows a workgroup; 0: a workgroup a row.
 // FAR: reads past the caches, with FULL alone.
 template <class T, int G, int NV, bool FULL, bool Q8, bool FAR>
@@ -188,7 +202,7 @@ __global__ void __launch_bounds__(G ? kOpThreads : 1024) rmsnorm_kernel(const Rm
         }
         row_sums<G>(sum, red, W / 64, turn);
         if constexpr (X::again) t = here(t);
-        const float r = 1.0f / __builtin_sqrtf(sum[0] / (float)H + a.eps);
+        const float r = reciprocal_root(sum[0] / (float)H + a.eps);
 #pragma unroll
         for (int j = 0; j < NV; ++j) {
             const uint32_t e = (j * W + t) * VE;
@@ -272,7 +286,7 @@ __global__ void __launch_bounds__(G ? kOpThreads : 1024) rmsnorm_backward_kernel
             }
             row_sums<G>(sums, red, W / 64, turn);
             if constexpr (X::again) t = here(t);
-            const float r = 1.0f / __builtin_sqrtf(sums[0] / (float)H + a.eps);
+            const float r = reciprocal_root(sums[0] / (float)H + a.eps);
             const float c = sums[1] / (float)H * r * r;
             now_h.forget(), now_g.forget();
 #pragma unroll

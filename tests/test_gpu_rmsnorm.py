@@ -352,3 +352,34 @@ def test_outputs_that_are_given_count_as_written():
     hc.rmsnorm(x, w, out=mid.detach())
     with pytest.raises(RuntimeError, match="modified by an inplace operation"):
         loss.backward()
+
+
+def test_the_reciprocal_root_is_rounded_once():
+    """Rows (1, k / 64): their squares' sum and mean are exact, and so are the
+    products with 1, so that y of the first and its weight's gradient are
+    1 / rms itself: off by half a step, and 2^-10 of one for a Newton step's
+    remainder (1.5 times the square of 2^-22)."""
+    k = torch.arange(4096, device="cuda")
+    h = torch.stack([torch.ones(4096, device="cuda"), k / 64], 1)
+    w = torch.ones(2, device="cuda")
+    want = 1 / ((1 + (k.double() / 64) ** 2) / 2).sqrt()
+    y = hc.rmsnorm(h, w, eps=0.0)
+    assert ((y[:, 0].double() - want).abs() <= (1 + 2.0 ** -10) * U * want).all()
+    for i in (0, 1, 63, 64, 777, 4095):
+        _, dw = hc.rmsnorm_backward(torch.ones(1, 2, device="cuda"), h[i:i + 1], w, eps=0.0)
+        assert abs(dw[0].double() - want[i]) <= (1 + 2.0 ** -10) * U * want[i]
+
+
+def test_magnitudes_near_the_ends_of_fp32():
+    """Rows whose mean of squares lies from 2^-120 to 2^120."""
+    w = torch.ones(64, device="cuda")
+    base = tensor(5, 64)
+    for e in (-60, -51, -50, -49, -30, 30, 49, 50, 51, 57):
+        x = (base * 2.0 ** e).view(1, 64)
+        check_forward(x, None, w, hc.rmsnorm(x, w, eps=0.0), None, eps=0.0)
+        dx, dw = hc.rmsnorm_backward(x * 2.0 ** -e, x, w, eps=0.0)
+        check_backward(x, x * 2.0 ** -e, None, w, dx, dw, eps=0.0)
+    # single powers of two, whose squares are exact down to 2^-148: y is 1
+    x = torch.ldexp(torch.ones(138), torch.arange(-74, 64)).view(-1, 1).cuda()
+    y = hc.rmsnorm(x, torch.ones(1, device="cuda"), eps=0.0)
+    assert torch.equal(y, torch.ones_like(y))
