@@ -123,7 +123,11 @@ struct Logits {
         for (int j = 0; j < NV; ++j) store_some<T, true>(p, at(j, lane), E, v[j]);
     }
     // To exp(x - max) over the L lanes; returns what makes them p: the
-    // reciprocal (1 ulp) of their sum.  Behind E there are zeros.
+    // reciprocal of their sum, an approximation and a Newton step (half a step
+    // off; all of a token's p carry it).  Behind E there are zeros.
+    // log2 e is one fp32 number, 1.3e-8 of the exponents off: 64 logits of
+    // deviation 3 have p with 7.8e-8 of rounding errors (relative, in the 2-norm), with
+    // an exact one 7.3e-8 for two more instructions a logit of about eight.
     __device__ __forceinline__ float softmax(int lane, int E) {
         float top = -INFINITY, sum = 0.0f;
         if (E < L * N)
@@ -161,7 +165,8 @@ struct Logits {
 #pragma unroll
             for (int i = 0; i < VE; ++i) sum += v[j][i];
         sum = join_lanes<L, LaneSum>(sum);
-        return sum == 0.0f ? 0.0f : __builtin_amdgcn_rcpf(sum);
+        const float inv = __builtin_amdgcn_rcpf(sum);
+        return sum == 0.0f ? 0.0f : fmaf(fmaf(-sum, inv, 1.0f), inv, inv);
     }
 };
 

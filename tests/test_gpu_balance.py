@@ -325,3 +325,18 @@ def test_replays(T):
             assert torch.equal(a, b), k
         check([y], [f], 8, out, d, g)
     del graph
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+def test_the_sums_reciprocal_is_rounded_once(dt):
+    """One token of E equal logits, whose exponentials are exactly 1 and their
+    sum E; the weight of the chosen expert is 1, so that the loss is p itself:
+    1 / E, off by half a step (and 2^-10 of one)."""
+    losses = []
+    for E in range(1, 1025):
+        x = torch.zeros(1, E, dtype=dt, device="cuda")
+        e = torch.zeros(1, 1, dtype=torch.int32, device="cuda")
+        losses.append(hc.balance_loss([x], [e], 1, expert_weight=1 / E).loss)
+    want = 1 / torch.arange(1, 1025, device="cuda", dtype=torch.float64)
+    got = torch.cat(losses).double()
+    assert ((got - want).abs() <= (1 + 2.0 ** -10) * U * want).all()
