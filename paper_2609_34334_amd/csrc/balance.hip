@@ -49,13 +49,6 @@ constexpr int kAhead = 2;      // tokens of a lane in flight
 // passes as the others, whatever the batches' lengths (eight batches of 9,800
 // to 32,768 tokens, 256 experts: 51 us with as many workgroups for each).
 constexpr size_t kBlocks = 512;
-// Batches of no more passes than this are a workgroup's each, which finishes
-// its batch without a second kernel.  256 tokens and 64 experts, two passes,
-// take 7.1 us instead of 8.9; 512 tokens, four, 10.0 instead of 8.9, but calls
-// this short wait for the host, which a launch and a workspace less spare
-// more (both directions: eager 20 us instead of 25, replayed 14.4 instead of
-// 12.4).
-constexpr size_t kOnePasses = 4;
 constexpr float kLog2e = 1.4426950408889634f;
 
 // Logits of a lane.  16 leave fewer lanes to exchange with but more registers
@@ -70,6 +63,29 @@ int lanes_of(int E, int logits) {
     while (l < 64 && l * logits < E) l *= 2;
     return l;
 }
+
+// Batches of no more passes than this are a workgroup's each, which finishes
+// its batch without a second kernel (and without a workspace).  A pass more
+// costs that workgroup 1.4 to 2.2 us, and 3.8 where one lane counts all of a
+// token's choices (up to 8 experts); the second kernel costs 3 us on the
+// device and 3 to 4.5 more of an eager call, which waits for the host.  One
+// batch forward, one kernel / two, replayed and eager, in us:
+//
+//   lanes, experts  passes  tokens  replayed      eager
+//   1, 8            2       2048    13.6 / 13.9   14.4 / 16.3
+//                   3       3072    17.4 / 14.1   18.3 / 17.8
+//   2, 16           3       1536    13.3 / 11.5   14.2 / 17.7
+//                   4       2048    16.1 / 11.7   16.9 / 17.9
+//   4, 32           3       768     12.1 / 10.4   13.5 / 16.8
+//                   4       1024    14.5 / 10.6   15.2 / 17.9
+//   8, 64           4       512     10.0 /  9.0   13.5 / 17.7
+//                   6       768     12.8 /  9.2   13.6 / 17.6
+//   64, 1024        4       64      12.6 / 10.9   13.5 / 17.8
+//                   6       96      16.4 / 11.1   17.2 / 17.8
+//
+// Up to the limits an eager call gains twice what a replayed one loses, or
+// more; both go one way, as a replay has to have the eager call's bits.
+size_t one_passes(int lanes) { return lanes < 2 ? 2 : lanes < 8 ? 3 : 4; }
 
 // Choice i behind `experts`, -1 where it is no expert.
 __device__ __forceinline__ int choice(const BalanceArgs &a, const char *experts, uint32_t i) {
@@ -500,11 +516,12 @@ size_t over(size_t n, size_t d) { return (n + d - 1) / d; }
 }  // namespace
 
 void balance_blocks(const size_t *tokens, int E, hoccl_dtype_t dt, int batches, uint32_t *first) {
-    const size_t rows = rows_of(kThreads, lanes_of(E, logits_of(E, dt, false)));
+    const int lanes = lanes_of(E, logits_of(E, dt, false));
+    const size_t rows = rows_of(kThreads, lanes);
     size_t all = 0, longest = 0;
     for (int b = 0; b < batches; ++b) all += over(tokens[b], rows), longest = std::max(longest, tokens[b]);
     first[0] = 0;
-    if (longest <= rows * kOnePasses) {
+    if (longest <= rows * one_passes(lanes)) {
         for (int b = 0; b < batches; ++b) first[b + 1] = (uint32_t)(b + 1);
         return;
     }

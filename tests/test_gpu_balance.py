@@ -340,3 +340,17 @@ def test_the_sums_reciprocal_is_rounded_once(dt):
     want = 1 / torch.arange(1, 1025, device="cuda", dtype=torch.float64)
     got = torch.cat(losses).double()
     assert ((got - want).abs() <= (1 + 2.0 ** -10) * U * want).all()
+
+
+@pytest.mark.parametrize("dt", [torch.float32, torch.bfloat16], ids=["fp32", "bf16"])
+@pytest.mark.parametrize("E,T", [(5, 2047), (5, 2049), (8, 3000), (8, 4096), (13, 1536), (16, 2048), (16, 1537), (30, 769),
+                                 (32, 1024), (64, 512), (64, 513)])
+def test_around_the_batches_of_one_workgroup(E, T, dt):
+    """Few experts, about as many tokens as one workgroup takes, and a short
+    batch beside them."""
+    index = torch.int64 if T % 2 else torch.int32
+    xs, es = zip(*[batch(E + T + b, n, E, 3, dt, index, 0.1) for b, n in enumerate((T, 33))])
+    xs, es = list(xs), list(es)
+    out = hc.balance_loss(xs, es, 1, **WEIGHTS)
+    g = torch.tensor([2.0, -0.5], device="cuda")
+    check(xs, es, 1, out, hc.balance_loss_backward(xs, es, out.coef, g), g)

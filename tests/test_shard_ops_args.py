@@ -234,6 +234,22 @@ def test_balance_workspace():
     assert L.hoccl_balance_workspace((ctypes.c_size_t * 1)(16), 1, ctypes.byref(options()), None) == BAD
 
 
+@pytest.mark.parametrize("dt,experts,most", [
+    (hc.FP32, 1, 2048), (hc.FP32, 8, 2048), (hc.FP32, 9, 1536), (hc.FP32, 16, 1536), (hc.FP32, 32, 768), (hc.FP32, 64, 512),
+    (hc.FP32, 256, 128), (hc.FP32, 1024, 64), (hc.BF16, 8, 2048), (hc.BF16, 32, 768), (hc.BF16, 128, 256),
+    (hc.BF16, 256, 256), (hc.BF16, 512, 128)])
+def test_balance_batches_of_one_workgroup(dt, experts, most):
+    """The longest batch that one workgroup finishes, which needs no
+    workspace: a few passes, fewer where one lane counts for a token."""
+    n = ctypes.c_size_t()
+    o = options(logits_dtype=dt, experts=experts, topk=1, ranks=1)
+    for tokens, some in ((most, False), (most + 1, True)):
+        for others in ((), (1, most)):
+            t = (*others, tokens)
+            assert L.hoccl_balance_workspace((ctypes.c_size_t * len(t))(*t), len(t), ctypes.byref(o), ctypes.byref(n)) == OK
+            assert (n.value > 0) == some
+
+
 @pytest.mark.parametrize("coef,dlogits", [(0, 4 * P), (3 * P, 0), (3 * P, P), (3 * P, 2 * P), (3 * P, 3 * P), (3 * P, 4 * P + 2)])
 def test_balance_backward_arguments(coef, dlogits):
     vp = ctypes.c_void_p * 1
