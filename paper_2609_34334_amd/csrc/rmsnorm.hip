@@ -28,10 +28,8 @@
 // Where rows fill their last vectors the backward pass reads and writes past
 // the caches (105 us otherwise, 94 so, at 16384 x 4096).  The forward pass
 // writes past them (4096 x 2048 into 8 bits 12.5 and 11.5 us, 8192 x 4096 50.8
-// and 50.0); it reads through them, as its inputs have mostly just been made,
-// but where the call moves more than the 256 MB that the last of them holds:
-// 8192 x 4096 takes 43 us instead of 50, 4096 x 2048, 59 MB, would take 12.7
-// instead of 11.1.
+// and 50.0); it reads through them where its inputs may still be there, past
+// them in large calls (kFarBytes).
 //
 // Bound by memory: 8 bytes an element (bf16 with a residual: 6.3 TB/s at 8192 x
 // 4096), 7 with y in 8 bits; backward 8 bytes (6.3 TB/s at 16384 x 4096) and the
@@ -423,7 +421,25 @@ const void *with_shape(hoccl_dtype_t dt, Shape s, F &&f) {
 
 }  // namespace
 
-constexpr unsigned long long kCacheBytes = 256ull << 20;
+// Calls of more bytes read past the caches: half of what the last of them (256
+// MiB) holds.  Rows of whole vectors, us with plain reads / past the caches,
+// where a call finds its inputs: nowhere (many tensors in turn), in what three
+// calls in turn leave, or all of them (the same tensors again):
+//
+//   bf16 with a residual   64 MB  14.5 / 13.1   10.9 / 13.1    9.3 / 12.4
+//                         128     25.4 / 23.5   22.5 / 22.7   20.1 / 22.7
+//                         160     31.2 / 27.4   31.0 / 26.8   24.8 / 26.9
+//                         260     49.9 / 42.4   50.7 / 43.5   41.6 / 44.5
+//   fp32                   64     14.6 / 13.9   11.0 / 13.0   10.9 / 12.8
+//                         128     25.3 / 24.5   25.4 / 23.1   20.6 / 23.6
+//                         256     49.6 / 49.1   47.8 / 46.9   39.0 / 41.5
+//   y in 8 bits            59     13.3 / 13.0   11.8 / 13.1   10.0 / 12.5
+//                         160     30.8 / 29.6   29.5 / 29.4   27.9 / 29.0
+//                         256     49.5 / 47.7   48.7 / 46.2   41.6 / 47.2
+//
+// The middle one, a step's calls one after another, crosses at about 128 MB, for
+// y in 8 bits at 160.
+constexpr unsigned long long kFarBytes = 128ull << 20;
 
 // Threads of a CU's workgroups in the forward pass: what it holds.  A quarter
 // of them: 48.5 us instead of 44.9 at 8192 x 4096, 14.1 instead of 12.6 at 4096
@@ -446,7 +462,7 @@ unsigned long long rmsnorm_workgroups(size_t rows, size_t hidden, hoccl_dtype_t 
 }
 
 hipError_t launch_rmsnorm(RmsArgs a, hoccl_dtype_t dt, unsigned long long bytes, int wg, hipStream_t s) {
-    const bool far = bytes > kCacheBytes;  // with FULL alone
+    const bool far = bytes > kFarBytes;  // with FULL alone
     const Shape sh = shape_of(a.hidden, dt);
     const void *k = with_shape(dt, sh, [&](auto type, auto g, auto n, auto full) -> const void * {
         using T = decltype(type);
