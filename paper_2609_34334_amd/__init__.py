@@ -24,7 +24,7 @@ LIB_PATH = os.path.join(_HERE, "libhoccl.so")
 for _path in (LIB_PATH, os.path.join(_HERE, "_tensors.so")):
     if not os.path.exists(_path):
         raise ImportError(
-            f"{_path} is not built; run `python -m paper_2609_34334_amd.build` "
+            f"{_path} is not built; run `python {os.path.join(_HERE, 'build.py')}` "
             "(or __graft_entry__.build()) first")
 
 from . import _tensors  # noqa: E402  (csrc/tensors.cpp)

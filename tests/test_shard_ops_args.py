@@ -1,6 +1,11 @@
 """The operators' refusals (CPU: bad arguments are found before a device is
 touched), through the C ABI with made-up pointers and through Python."""
 import ctypes
+import os
+import re
+import shutil
+import subprocess
+import sys
 
 import pytest
 import torch
@@ -279,3 +284,24 @@ def test_balance_python():
         hc.balance_loss([torch.zeros(4)], e, 4)
     with pytest.raises(ValueError, match="coef"):
         hc.balance_loss_backward(x, e, torch.zeros(2, 8))
+
+
+# ---- what is not built ----------------------------------------------------------
+
+
+@pytest.mark.parametrize("there", [[], ["libhoccl.so"]])
+def test_the_import_names_a_build_command_that_runs(tmp_path, there):
+    """Without one of the two built files the import says how to build them;
+    the command does not need the package that cannot be imported yet."""
+    package = tmp_path / "paper_2609_34334_amd"
+    package.mkdir()
+    home = os.path.dirname(hc.__file__)
+    for name in ["__init__.py", "build.py", *there]:
+        shutil.copy(os.path.join(home, name), package)
+    env = dict(os.environ, PYTHONPATH=str(tmp_path), HIPCC="/bin/false", CXX="/bin/false")
+    r = subprocess.run([sys.executable, "-c", "import paper_2609_34334_amd"], cwd=tmp_path, env=env, capture_output=True,
+                       text=True)
+    assert r.returncode != 0 and "is not built" in r.stderr
+    command = re.search("`python (.*?)`", r.stderr).group(1)
+    r = subprocess.run([sys.executable, *command.split()], cwd=tmp_path, env=env, capture_output=True, text=True)
+    assert r.returncode != 0 and "compiling" in r.stderr and "is not built" not in r.stderr
