@@ -176,6 +176,18 @@ def test_formulas(param, grad, bits, shift):
 
 
 @pytest.mark.parametrize("bits", [32, 8])
+@pytest.mark.parametrize("grad", ["fp32", "bf16"])
+def test_copies_of_bf16_parameters(grad, bits):
+    """A copy is asked for where the parameters are bf16 themselves: the same
+    bits."""
+    c = Case(SIZES, 13, "bf16", grad, bits, copy=True, shift=1)
+    before = c.snapshot()
+    c.step()
+    torch.cuda.synchronize()
+    check(c, before)
+
+
+@pytest.mark.parametrize("bits", [32, 8])
 def test_from_the_first_step_on(bits):
     """Steps 1, 2, 3 from zero states, the gradients scaled on the device."""
     c = Case([4100, 77], 5, bits=bits, fresh=True)

@@ -354,3 +354,22 @@ def test_around_the_batches_of_one_workgroup(E, T, dt):
     out = hc.balance_loss(xs, es, 1, **WEIGHTS)
     g = torch.tensor([2.0, -0.5], device="cuda")
     check(xs, es, 1, out, hc.balance_loss_backward(xs, es, out.coef, g), g)
+
+
+@pytest.mark.parametrize("T,E,R,dt,index", [
+    (40_000, 64, 1, torch.float32, torch.int64), (20_000, 200, 3, torch.float32, torch.int64),
+    (20_000, 130, 1, torch.float32, torch.int32), (9_000, 500, 1, torch.float32, torch.int32),
+    (9_000, 1024, 2, torch.float32, torch.int64), (20_000, 200, 3, torch.bfloat16, torch.int64),
+    (600_001, 8, 1, torch.float32, torch.int64), (600_001, 5, 1, torch.bfloat16, torch.int32),
+    (300_001, 16, 1, torch.float32, torch.int32), (300_001, 13, 1, torch.bfloat16, torch.int64),
+    (150_001, 30, 1, torch.float32, torch.int64), (150_001, 32, 1, torch.bfloat16, torch.int32),
+    (6_000, 8, 3, torch.float32, torch.int32), (3_000, 24, 4, torch.bfloat16, torch.int64)])
+def test_many_tokens_of_every_kind(T, E, R, dt, index):
+    """Several workgroups a batch, and several passes of one, for 1 to 64
+    lanes a token in either type."""
+    ranks = 8 if E % 8 == 0 else 1
+    xs, es = zip(*[batch(60 + b, T - 7 * b, E, 4, dt, index, 0.1) for b in range(R)])
+    xs, es = list(xs), list(es)
+    out = hc.balance_loss(xs, es, ranks, **WEIGHTS)
+    assert hc.last_stats()["reduce_launches"] == 2
+    check(xs, es, ranks, out, hc.balance_loss_backward(xs, es, out.coef))

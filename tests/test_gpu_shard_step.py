@@ -56,6 +56,45 @@ def test_sharded_steps(bits):
             assert ((got.double() - p).abs() <= step * 12 * lr).all()
 
 
+def test_sharded_8bit_steps_from_what_each_finds():
+    """The same with 8-bit states, every step against the formulas in 64 bits
+    from the states that the step before has left: to the roundings of fp32."""
+    R, n = 4, 3001
+    whole = randn(1, R * n, scale=0.1)
+    shards = [whole[r * n:(r + 1) * n].clone() for r in range(R)]
+    state = hc.adamw_state(shards, bits=8)
+    copies = [torch.empty(n, dtype=torch.bfloat16, device="cuda") for _ in range(R)]
+    lr, (b1, b2), decay, eps = 1e-2, (0.9, 0.99), 0.1, 1e-8
+
+    def held(codes, scales):
+        each = [s.repeat_interleave(128)[:n] for s in scales]
+        return torch.cat([q.float() * s for q, s in zip(codes, each)])
+
+    for step in range(1, 6):
+        p, m, root = torch.cat(shards).double(), held(state[0], state[2]).double(), held(state[1], state[3])
+        v = (root * root).double()                       # as the kernel takes it, in fp32
+        mine = hc.reduce_scatter([randn(10 * step + r, R * n, dt=torch.bfloat16) for r in range(R)])
+        hc.adamw(shards, mine, *state, step=step, lr=lr, betas=(b1, b2), eps=eps, weight_decay=decay, copies=copies,
+                 grad_scale=torch.tensor([1 / R], device="cuda"))
+        torch.cuda.synchronize()
+        g = torch.cat(mine).double() / R
+        m1, v1 = b1 * m + (1 - b1) * g, b2 * v + (1 - b2) * g * g
+        den, rate = v1.sqrt() / math.sqrt(1 - b2 ** step) + eps, lr / (1 - b1 ** step)
+        want = p * (1 - lr * decay) - rate * m1 / den
+        # m: scale and product, beta, its product and the sum; the update: rate, its product, root (half of v's 6.1,
+        # and 1), factor, product, eps and sum, reciprocal and product, last difference; the parameter: 1 - lr wd, product, sum
+        err_m = 4.1 * U * (b1 * m.abs() + (1 - b1) * g.abs())
+        err = 3.1 * U * p.abs() + 13.1 * U * (rate * m1 / den).abs() + rate * err_m / den + 1e-30
+        got = torch.cat(shards)
+        assert ((got.double() - want).abs() <= err).all(), step
+        assert torch.equal(torch.cat(copies), got.bfloat16())
+        # the states that it leaves: half a step of e4m3, and the root's floor
+        for x, codes, scales, floor in ((m1, state[0], state[2], 0.0), (v1.sqrt(), state[1], state[3], 2.0 ** -9)):
+            each = torch.cat([s.repeat_interleave(128)[:n] for s in scales]).double()
+            now = held(codes, scales).double()
+            assert ((now - x).abs() <= (2.0 ** -4 + 20 * U) * x.abs() + (2.0 ** -10 + floor) * each + err_m).all(), step
+
+
 def test_sequence_parallel_norm():
     """reduce-scatter of partial outputs -> residual + RMS norm in 8 bits on
     each rank's rows -> all-gather of the bytes and of the scales; the
