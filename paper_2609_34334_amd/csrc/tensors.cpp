@@ -179,9 +179,15 @@ PyObject *wrote(PyObject *, PyObject *args) {
             if (PyTuple_GET_ITEM(args, i) == Py_None) continue;
             PyObject *seq = PySequence_Fast(PyTuple_GET_ITEM(args, i), "a list of tensors is needed");
             if (!seq) return nullptr;
-            const bool fine = each(seq, [](Py_ssize_t, const at::Tensor &t) {
-                // Those of inference mode have no version.
-                if (!t.is_inference()) t.unsafeGetTensorImpl()->bump_version();
+            // Views share their version; of neighbours that do, one is enough
+            // (150 shards of five flat buffers each: 7 us, 2 so).
+            const c10::VariableVersion *last = nullptr;
+            const bool fine = each(seq, [&](Py_ssize_t, const at::Tensor &t) {
+                at::TensorImpl *impl = t.unsafeGetTensorImpl();
+                const c10::VariableVersion &version = impl->version_counter();
+                if (!version.enabled()) return true;  // of inference mode
+                if (!last || std::memcmp((const void *)last, (const void *)&version, sizeof version)) impl->bump_version();
+                last = &version;
                 return true;
             });
             Py_DECREF(seq);

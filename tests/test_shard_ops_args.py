@@ -86,6 +86,12 @@ def test_versions_of_written_tensors():
     versions = a._version, b._version
     hc._tensors.wrote([a, c], None, (b, a))
     assert (a._version, b._version) == (versions[0] + 2, versions[1] + 1)
+    flat, alone = torch.zeros(12), torch.zeros(2)
+    views = [*flat.split(4), alone, flat[1:3]]                        # views share the version of what they are cut from
+    versions = flat._version, alone._version
+    hc._tensors.wrote(views)
+    assert flat._version > versions[0] and alone._version == versions[1] + 1
+    assert all(v._version == flat._version for v in views if v is not alone)
     with pytest.raises(TypeError):
         hc._tensors.wrote([a, None])
     with pytest.raises(TypeError):
