@@ -594,7 +594,7 @@ typedef struct {
  * at least, never as zero.  A rounding to 8 bits loses changes of less than
  * half a step, 1/16 of a value: with beta2 near 1 a v that is a block's
  * largest follows its gradients, the others follow in such steps.  bf16
- * parameters are rounded likewise (2^-9): small updates need fp32
+ * parameters are rounded likewise (2^-8): small updates need fp32
  * parameters, whose bf16 `copy` is then what the all-gather sends.  eps is 0
  * or at least 2^-126.  Tensors of no elements are skipped; 76 tensors share
  * a launch. */

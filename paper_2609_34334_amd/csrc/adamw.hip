@@ -19,8 +19,8 @@
 // states are those of the formulas taken one operation at a time in fp32.
 //
 // Bound by memory: 28 bytes an element (fp32 parameters and states, bf16
-// gradients and copies; 25.2M elements in 118 us, 5.95 TB/s), 16.1 with 8-bit
-// states (63 us, 6.5 TB/s, part of it from the caches).  Many small tensors
+// gradients and copies; 25.2M elements in 117 us, 6.0 TB/s), 16.1 with 8-bit
+// states (62 us, 6.5 TB/s, part of it from the caches).  Many small tensors
 // are bound by the launches, of kAdamSegs tensors each, and by the host.
 #include <algorithm>
 #include <type_traits>
@@ -33,11 +33,11 @@
 namespace hoccl {
 namespace {
 
-// Elements of a lane's vector, and vectors of a thread in a tile.  25.2M
-// elements: 32 bits 114 us with one vector of four, 119 with two; 8 bits, where
-// two share the work on their scales, 82 and 77.  With bf16 parameters one of
-// eight makes wider accesses: 49 us instead of 52, but 65 instead of 59 with
-// fp32 ones, whose 32 bytes a lane are two accesses with gaps.
+// Elements of a lane's vector, and vectors of a thread in a tile.  With 25.2M
+// elements two vectors of four take 4 % longer than one in 32 bits, and 6 % less
+// in 8 bits, where two share the work on their scales.  With bf16 parameters
+// one of eight makes wider accesses: 6 % less, but 10 % more with fp32 ones,
+// whose 32 bytes a lane are two accesses with gaps.
 template <class TP, bool Q8>
 constexpr int kVE = Q8 && TP::size == 2 ? 8 : 4;
 template <class TP, bool Q8>
@@ -45,9 +45,9 @@ constexpr int kU = Q8 ? 8 / kVE<TP, Q8> : 1;
 template <bool Q8>
 constexpr uint32_t kTile = kOpThreads * (Q8 ? 8 : 4);
 
-// Every byte is used once a step: reads and writes are non-temporal.  With
-// plain ones 25.2M elements took 136 us instead of 119 (32 bits).  The codes
-// of 8-bit states, four bytes a lane, are better off plain (77 and 74 us).
+// Every byte is used once a step: reads and writes are non-temporal (25.2M
+// elements, 32 bits: plain ones take 14 % longer).  The codes of 8-bit states,
+// four bytes a lane, are plain (non-temporal 4 % longer).
 constexpr bool kNT = true;
 
 struct Hyper {
@@ -61,7 +61,8 @@ __device__ __forceinline__ float step_one(const Hyper &h, float p, float g, floa
     v = v * h.b2 + g * g * h.c2;
     r = __builtin_sqrtf(v);
     // The reciprocal (1 ulp) instead of a division, whose 11 instructions 25.2M
-    // elements of 8-bit states felt: 71.7 us instead of 67.9.  The divisor is
+    // elements of 8-bit states felt: 6 % longer.  The update's error hardly
+    // shows in the parameter, which is larger by far.  The divisor is
     // zero or normal (eps is, and the smallest root is 2^-75).
     return p * h.decay - h.rate * m * __builtin_amdgcn_rcpf(r * h.root + h.eps);
 }

@@ -27,11 +27,13 @@
 // of the workgroups, a number that goes by the sizes alone, are added in order
 // by one workgroup a batch.
 //
-// Memory's part is logits and choices read once and gradients written; what
-// holds the forward pass at many tokens is its arithmetic as well, some 8
-// instructions a logit (eight batches of 9,800 to 32,768 tokens, 256 experts,
-// bf16: 25.6 us for 93 MB and 6.6 for the sums' end, backward 30 us for 180 MB),
-// at few tokens the launches and the latency of the last sum.
+// Memory's part is logits and choices read once and gradients written; the
+// forward pass at many tokens has as much arithmetic, some 8 instructions a
+// logit, and four waves a SIMD do not hide one behind the other (eight batches of
+// 9,800 to 32,768 tokens, 256 experts, bf16: 25.4 us, where memory alone and
+// arithmetic alone would take 15 each, and 6.5 for the sums' end; backward 29.4
+// us for 180 MB).  At few tokens it is the launches and the latency of the last
+// sum.
 #include <algorithm>
 #include <type_traits>
 
@@ -44,16 +46,18 @@ namespace {
 constexpr int kThreads = 512;  // of the forward pass's first kernel
 constexpr int kWaves = kThreads / 64;
 constexpr int kAhead = 2;      // tokens of a lane in flight
-// Workgroups of the forward pass, and half of them at most for one batch:
-// two a CU, which is what its registers hold.  Every workgroup makes as many
-// passes as the others, whatever the batches' lengths (eight batches of 9,800
-// to 32,768 tokens, 256 experts: 51 us with as many workgroups for each).
+// Workgroups of the forward pass, and half of them at most for one batch: two a
+// CU, which is what its registers hold (of fp32 over 512 experts one alone, so
+// two rounds).  Every workgroup makes as many passes as the others, whatever the
+// batches' lengths (eight batches of 9,800 to 32,768 tokens, 256 experts: 2 us
+// less than with as many workgroups for each), and whole ones, so that places
+// may stay empty (there 448 of 512 are taken).
 constexpr size_t kBlocks = 512;
 constexpr float kLog2e = 1.4426950408889634f;
 
 // Logits of a lane.  16 leave fewer lanes to exchange with but more registers
-// for fewer waves: forward, 8 x 16384 tokens and 256 experts take 22.5 us with
-// 16 and 26.5 with 8 in bf16, 41 and 32 in fp32, of 128 experts 20.9 and 16.5 in
+// for fewer waves: forward, 8 x 16384 tokens and 256 experts take 15 % less with
+// 16 than with 8 in bf16, but 28 % more in fp32, and of 128 experts 27 % more in
 // bf16.
 int logits_of(int E, hoccl_dtype_t dt, bool backward) {
     return E > 512 || (!backward && dt == HOCCL_BF16 && E > 128) ? 16 : 8;
@@ -379,8 +383,9 @@ __global__ void __launch_bounds__(kThreads) balance_kernel(BalanceArgs) {
 
 // The same from the sums of a batch's blocks, rows of the table.  Lots of rows
 // are added side by side, four columns a thread and twelve rows of them in
-// flight, then the lots in order: one row and column after another, 64 blocks
-// took 35 us, all latency; a column a thread 11 (256 experts), so 8.
+// flight, then the lots in order: 6.5 us, all latency (one row and column after
+// another took four times as long, a column a thread 1.4 times, for 64 blocks of
+// 256 experts).
 constexpr int kFinishThreads = 1024;
 constexpr int kLotAhead = 12;
 __global__ void __launch_bounds__(kFinishThreads) balance_finish_kernel(BalanceArgs) {

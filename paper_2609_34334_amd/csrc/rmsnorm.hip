@@ -18,22 +18,22 @@
 // one wave, with no exchange through LDS) hold a row in registers, a vector
 // of 16 bytes each up to 1024 of them, so that what is read is read once.  The
 // next row's reads are under way while a row is summed and written.  One
-// vector a thread keeps the registers few and the waves many: with up to four
-// (256 threads for 4096 elements, one wave for 2048) the norm of 8192 x 4096
-// took 58 us instead of 47, of 4096 x 2048 into 8 bits 23.5 instead of 17, the
-// gradients at 16384 x 4096 164 instead of 117; with the reads ahead and what
-// follows these are 42, 11 and 85 now.  Sums are in fp32, in an order that
-// goes by the row's length alone.
+// vector a thread keeps the registers few and the waves many: up to four (256
+// threads for 4096 elements, one wave for 2048), without the reads ahead, cost
+// 23 % at 8192 x 4096, 38 % into 8 bits at 4096 x 2048 and 40 % in the gradients
+// at 16384 x 4096.  Sums are in fp32, in an order that goes by the row's length
+// alone.
 //
 // Where rows fill their last vectors the backward pass reads and writes past
-// the caches (105 us otherwise, 94 so, at 16384 x 4096).  The forward pass
-// writes past them (4096 x 2048 into 8 bits 12.5 and 11.5 us, 8192 x 4096 50.8
-// and 50.0); it reads through them where its inputs may still be there, past
-// them in large calls (kFarBytes).
+// the caches (16384 x 4096: 12 % longer otherwise).  The forward pass writes
+// past them (8 % longer otherwise at 4096 x 2048 into 8 bits, 2 % at 8192 x
+// 4096); it reads through them where its inputs may still be there, past them
+// in large calls (kFarBytes).
 //
-// Bound by memory: 8 bytes an element (bf16 with a residual: 6.3 TB/s at 8192 x
-// 4096), 7 with y in 8 bits; backward 8 bytes (6.3 TB/s at 16384 x 4096) and the
-// partial sums of the weight's gradient.
+// Bound by memory: 8 bytes an element (bf16 with a residual: 42 us, 6.4 TB/s at
+// 8192 x 4096), 7 with y in 8 bits (11.5 us, 5.1 TB/s at 4096 x 2048, two rows a
+// workgroup); backward 8 bytes and the partial sums of the weight's gradient (82
+// and 5 us, 6.2 TB/s, at 16384 x 4096).
 #include <algorithm>
 #include <type_traits>
 
@@ -54,28 +54,30 @@ __device__ __forceinline__ void load_weights(const void *w, int bf16, uint32_t e
 }
 
 // What a thread holds of a row: NV vectors.  FULL: the vectors of the row's
-// threads end where it does (checking for it in the loop, the gradients at
-// 16384 x 4096 took 101 us instead of 95).
+// threads end where it does (checking for it in the loop costs the gradients at
+// 16384 x 4096 6 %).
 template <class T, int NV, bool FULL>
 struct Shaped {
     static constexpr int VE = kVE<T>, N = NV * VE;
     // Longer rows (over 8192 bf16 elements) have no registers for the next
     // one; the longest none for the weights, which they read again, nor, in the
     // backward pass, for the residual's gradient, which is read last, and the
-    // weights' gradients, which stay in LDS (64 MB of 20000 bf16: 57 us instead
-    // of 124; but of 12288 fp32, whose 16 elements a thread fit, 56 instead of
-    // 48).
+    // weights' gradients, which stay in LDS (rows of 20000 bf16 take 2.2 times as
+    // long otherwise; but rows of 12288 fp32, whose 16 elements a thread fit, 17 %
+    // longer so).
     static constexpr bool ahead = N <= 8, lean = N >= 32, keep_weights = N <= 16;
     // The offsets of many vectors, their comparisons with the row's end and their
-    // addresses would be kept over the loop, in more registers than the row
-    // (64 MB of 20000 fp32: 133 us, and the gradients 139): they are made anew
-    // for every row (49, 87), of the longest again after its sums (41, 50).
+    // addresses would be kept over the loop, in more registers than the row: they
+    // are made anew for every row (20000 fp32: 2.7 times as long otherwise, the
+    // gradients 1.6 times), of the longest again after its sums (16 % and 43 %
+    // less).  The gradients of 8193 to 16384 elements whose last vectors are not
+    // whole still keep 20 bytes of them a lane in scratch memory (bf16), 8 (fp32).
     static constexpr bool anew = NV >= 4, again = NV >= 8;
     Raw<16> v[NV];
     // W threads a row, of which this is number t.
     // Lines that two rows or two vectors share are read twice: through the
-    // caches, whatever NT says (the gradients of 64 MB of 5003 bf16 80 us past
-    // them and 63 so, the norm of 2049 65 and 52).
+    // caches, whatever NT says (past them the gradients of 5003 bf16 take 27 %
+    // longer, the norm of 2049 25 %).
     template <bool NT>
     __device__ __forceinline__ void load(const void *p, uint64_t row, uint32_t H, uint32_t W, uint32_t t) {
         const char *at = (const char *)p + row * H * T::size;
@@ -175,8 +177,8 @@ __global__ void __launch_bounds__(G ? kOpThreads : 1024) rmsnorm_kernel(const Rm
         float h[NV][VE], sum[1] = {0.0f};
         if (!X::ahead) load(row);
         // The next row's reads go out before this one's are waited for, or,
-        // where y is not in 8 bits, after: 8192 x 4096 in 8 bits 38.5 us and
-        // 42.1, else 49.9 and 47.6.
+        // where y is not in 8 bits, after: at 8192 x 4096 the other order costs 9 %
+        // in 8 bits and 5 % else.
         X now = x, now_res = res;
         if (Q8 && X::ahead && row + step < a.rows) load(row + step);
         now.settle(H, W, t);
@@ -442,14 +444,13 @@ const void *with_shape(hoccl_dtype_t dt, Shape s, F &&f) {
 constexpr unsigned long long kFarBytes = 128ull << 20;
 
 // Threads of a CU's workgroups in the forward pass: what it holds.  A quarter
-// of them: 48.5 us instead of 44.9 at 8192 x 4096, 14.1 instead of 12.6 at 4096
-// x 2048 into 8 bits.
+// of them: 8 % longer at 8192 x 4096, 12 % at 4096 x 2048 into 8 bits.
 constexpr unsigned kForwardThreads = 2048;
 // Workgroups of the backward pass, and partial sums: as many for each of 256
-// CUs as make about 512 threads.  16384 x 4096 takes 92 us so and 99 with 1024
+// CUs as make about 512 threads.  16384 x 4096 takes 8 % longer with 1024
 // threads; but rows under 512 threads whose last vectors are not whole leave
-// lanes idle and wait more (64 MB of 640 bf16: 79 us with 512, 60 with 1024;
-// of 5003, 640 threads, 60.5 and 63.5).
+// lanes idle and wait more (640 bf16: 24 % less with 1024; 5003, 640 threads, 5
+// % more).
 size_t backward_groups(Shape s) {
     const int threads = group_of(s), most = s.full || threads >= 512 ? 512 : 1024;
     return 256 * (size_t)std::max(1, (most + threads / 2) / threads);
