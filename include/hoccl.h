@@ -606,7 +606,8 @@ hoccl_status_t hoccl_adamw(const hoccl_adamw_tensor_t *tensors, int count, const
  *   h = x + residual, rounded to dtype (h = x where residual is NULL)
  *   y = h * weight / sqrt(mean(h * h) + eps)
  * The squares' sum is fp32 too: a row whose sum passes its range (magnitudes
- * of 2^64 / sqrt(hidden) and more) has no y to rely on.
+ * of 2^64 / sqrt(hidden) and more; with eps = 0 under 2^-63 as well) has no y
+ * to rely on.
  * residual_out (or NULL) receives h.  y is of dtype; with `scale` it is e4m3
  * bytes, ceil(hidden / HOCCL_BLOCK) scales a row, the last block of a row
  * short where hidden is not a multiple: bytes an all-gather moves as

@@ -136,14 +136,13 @@ __device__ __forceinline__ void row_sums(float (&v)[M], float (*red)[16][M], uin
 // 1 / sqrt(v), rounded once: the approximation (1 ulp) and a Newton step on it,
 // r + r (1 - v r r) / 2, whose difference is taken in two parts, from the
 // rounded product v r and from its rounding.  (1 / sqrtf rounds twice and takes
-// more instructions.)  Values near and in the subnormal range are scaled; of
-// infinity it is 0.
+// more instructions.)  Values near and in the subnormal range are scaled.
 __device__ __forceinline__ float reciprocal_root(float v) {
     const bool tiny = v < 0x1p-100f;
     if (tiny) v *= 0x1p100f;
     const float r = __builtin_amdgcn_rsqf(v), h = v * r;
     const float e = fmaf(-fmaf(v, r, -h), r, fmaf(-h, r, 1.0f));
-    const float s = v < INFINITY ? fmaf(0.5f * r, e, r) : r;
+    const float s = e == e ? fmaf(0.5f * r, e, r) : r;  // not of zero and infinity
     return tiny ? s * 0x1p50f : s;
 }
 

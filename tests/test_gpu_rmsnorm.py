@@ -383,3 +383,8 @@ def test_magnitudes_near_the_ends_of_fp32():
     x = torch.ldexp(torch.ones(138), torch.arange(-74, 64)).view(-1, 1).cuda()
     y = hc.rmsnorm(x, torch.ones(1, device="cuda"), eps=0.0)
     assert torch.equal(y, torch.ones_like(y))
+    # squares that vanish, or pass the range: 1 / rms is infinite, or 0
+    for dt in (torch.float32, torch.bfloat16):
+        x = torch.tensor([[2.0 ** -100] * 8, [2.0 ** 100] * 8], device="cuda").to(dt)
+        y = hc.rmsnorm(x, torch.ones(8, device="cuda"), eps=0.0)
+        assert torch.isposinf(y[0]).all() and (y[1] == 0).all()
